@@ -393,6 +393,126 @@ ql_status ql_train_step(const ql_train_model *M, const float *feats, const int32
                         int32_t quantize_output, float *loss, const ql_train_model *grads,
                         void *ws, size_t ws_bytes, void *stream);
 
+/* ---- a quantized state-space block ---------------------------------------------
+ * A recurrent layer of another kind on the same 8-bit activations: a norm that
+ * quantizes its result (ql_rms_norm), products with weights in 4 bits
+ * (ql_matmul4), a short causal convolution and a selective scan with their state
+ * carried from call to call.  Rows and sequences are fp32, fp16 or bfloat16
+ * (ql_type); parameters, statistics and states are fp32.  Rounding to the two
+ * narrow types is to the nearest, ties to even, once, where a value is stored.
+ *
+ * A tensor and its neighbours may be column slices of one buffer: `ld` and the
+ * strides count elements and are not bound to the widths.  Results must not
+ * overlap inputs unless a call says so (QL_EINVAL where it is seen). */
+typedef enum { QL_F32 = 0, QL_F16 = 1, QL_BF16 = 2 } ql_type;
+
+/* Root-mean-square norm of m rows of `cols` values (> 0), with the residual's
+ * addition:
+ *   v    = x + residual, rounded to the type (residual nullable: v = x)
+ *   rstd = (float)(1 / sqrt(sum v^2 / cols + eps)), in fp64; eps >= 0 finite
+ *   y    = (v rstd) weight, two fp32 roundings (weight [cols] nullable: ones)
+ * Results, each nullable but not all of them: sum = v; y rounded to the type;
+ * codes = the fp32 y quantized per row as ql_quantize_activations does
+ * (codes->rows = m, codes->cols = cols); rstd [m], for the backward pass.
+ * A row with a result that is not finite gets recovery factor NaN in codes
+ * (zero point 0, V' = 0), so products of it are NaN.  sum and y may each lie
+ * on x or residual exactly (the same pointer and leading dimension). */
+ql_status ql_rms_norm(ql_type type, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                      const float *weight, int64_t m, int64_t cols, double eps, void *sum,
+                      int64_t lds, void *y, int64_t ldy, const ql_qact *codes, float *rstd,
+                      void *stream);
+/* Its gradients, the quantizer not differentiated (as in ql_train_step): with
+ * g = weight dy and v, rstd as above,
+ *   dx = rstd g - v rstd^3 / cols sum(g v) + dsum   (the gradient at x and at
+ *        residual; dsum, nullable: the gradient arriving at sum)
+ *   dweight [cols] = sum over rows of dy (v rstd)   (fp32, nullable; written,
+ *        not added to; summed in a fixed order)
+ * dx may lie on dy, v or dsum exactly.  The workspace serves dweight. */
+size_t ql_rms_norm_backward_workspace(int64_t m, int64_t cols);
+ql_status ql_rms_norm_backward(ql_type type, const void *dy, int64_t lddy, const void *v,
+                               int64_t ldv, const float *rstd, const float *weight,
+                               const void *dsum, int64_t ldds, int64_t m, int64_t cols, void *dx,
+                               int64_t lddx, float *dweight, void *ws, size_t ws_bytes,
+                               void *stream);
+
+/* A matrix in 4 bits: each row in groups of 32, 64 or 128 columns, quantized
+ * independently with S = 15 from the group's range widened to hold 0, so that
+ * V' = round(Q V) - round(Q Vmin) lies in 0..15 and the zero point z =
+ * round(Q Vmin) in -15..0; recovered value (V' + z) q with q = (float)(R / 15)
+ * (an all-zero group: q = 1, z = 0, V' = 0).  Codes: rows of ld / 2 bytes, ld =
+ * cols rounded up to 128; in every 128 columns 16 little-endian 32-bit words, of
+ * which word 4 i + p (i, p in 0..3) holds columns 32 p + 8 i .. + 7: byte j the
+ * column j in its low half and j + 4 in its high half, each as V' - 8 in two's
+ * complement.  Columns [cols, ld) recover to 0.  zero and inv_q:
+ * [ld / group][rows rounded up to 16] (the rows past `rows` are not read into
+ * any result).  Device memory; codes and inv_q 16-byte, zero 4-byte aligned. */
+typedef struct {
+  uint8_t *codes;
+  int64_t rows, cols, ld;
+  int32_t group;
+  int8_t *zero;
+  float *inv_q;
+} ql_qmatrix4;
+/* src [rows][cols] fp32 into dst, whose arrays the caller allocated; values must
+ * be finite.  Offline step for weights. */
+ql_status ql_quantize4(const float *src, int64_t rows, int64_t cols, ql_qmatrix4 *dst,
+                       void *stream);
+/* Recovery: dst [rows][cols] fp32. */
+ql_status ql_dequantize4(const ql_qmatrix4 *q, float *dst, void *stream);
+/* Y [X->rows][W->rows] = recovered X times recovered W^T (+ bias [W->rows], fp32,
+ * nullable), Y of `type`: the products of a group are summed exactly, the groups
+ * in fp32.  X: per-vector codes (X->cols = W->cols, 16-byte aligned; X->sums is
+ * not read), from ql_rms_norm or ql_quantize_activations.  Any number of
+ * columns; up to 4194240 rows of X. */
+ql_status ql_matmul4(const ql_qmatrix4 *W, const ql_qact *X, const float *bias, ql_type type,
+                     void *Y, void *stream);
+/* The same from rows X [m][cols] of xtype, quantized on the fly per row (a row
+ * with a value that is not finite gives NaN).  Y may lie on X: X is read first. */
+size_t ql_quantized_matmul4_workspace(int64_t m, int64_t cols);
+ql_status ql_quantized_matmul4(const ql_qmatrix4 *W, ql_type xtype, const void *X, int64_t ldx,
+                               int64_t m, const float *bias, ql_type ytype, void *Y, void *ws,
+                               size_t ws_bytes, void *stream);
+
+/* Sequences of a batch: value (t, b, c) at data + t t_stride + b b_stride + c,
+ * whether they lie time-major or one utterance after the other. */
+typedef struct {
+  void *data;
+  int64_t t_stride, b_stride; /* elements, >= 0 */
+} ql_seq;
+/* Short causal convolution over time of every channel, T steps of B sequences of
+ * D channels (T <= 2^20, B <= 65535):
+ *   y_t = f(bias + sum_j w[j] x_{t - width + 1 + j}),  j = 0 .. width - 1 <= 7
+ * with f SiLU (silu = 1) or none (0); w [width][D], bias [D] nullable.  state
+ * [B][width - 1][D] fp32 holds the last width - 1 inputs, oldest first: state_in
+ * (nullable: zeros) before step 0, state_out (nullable) after the last one; they
+ * may be one buffer.  lengths [B] (device int32, nullable: T): sequence b ends
+ * after lengths[b] steps (taken as 0 or T where outside); its rows of y past
+ * that are left as they are, and its state is the one after its own last step. */
+ql_status ql_causal_conv(ql_type type, const ql_seq *x, const float *w, const float *bias,
+                         int32_t width, int32_t silu, int64_t T, int64_t B, int64_t D,
+                         const int32_t *lengths, const float *state_in, float *state_out,
+                         const ql_seq *y, void *stream);
+/* Selective scan: per channel `states` (1 .. 64) decaying states,
+ *   d = delta_t + delta_bias, through softplus where asked
+ *   h[n] = exp(d A[n]) h[n] + (d u_t) B_t[n]
+ *   y_t = (sum_n C_t[n] h[n] + D u_t) silu(z_t)
+ * u, delta, z (nullable: no gate) and y have `channels` values a step, Bm and Cm
+ * `states`, shared by the channels.  A [states][channels]; D and delta_bias
+ * [channels], nullable (zeros); state [B][states][channels] and lengths as in
+ * ql_causal_conv.  y may lie on u, delta or z exactly (same pointer and strides).
+ * Chaining calls through the state gives the values of one call to rounding. */
+typedef struct {
+  int64_t channels, states;
+  const float *A, *D, *delta_bias;
+  int32_t softplus;
+} ql_scan;
+size_t ql_selective_scan_workspace(int64_t channels, int64_t states, int64_t T, int64_t B);
+ql_status ql_selective_scan(ql_type type, const ql_scan *P, const ql_seq *u, const ql_seq *delta,
+                            const ql_seq *Bm, const ql_seq *Cm, const ql_seq *z, int64_t T,
+                            int64_t B, const int32_t *lengths, const float *state_in,
+                            float *state_out, const ql_seq *y, void *ws, size_t ws_bytes,
+                            void *stream);
+
 /* ---- misc -------------------------------------------------------------------- */
 /* Synchronizes `stream`, then reports QL_ETIMEOUT if a persistent kernel of the
  * last layer / model forward call (8-bit or fp32) that used this

@@ -1493,4 +1493,348 @@ ql_status ql_train_step(const ql_train_model *M, const float *feats, const int32
   return QL_OK;
 }
 
+// ------------------------------------------- a quantized state-space block
+namespace {
+
+constexpr int64_t kMaxDim = 2147483647;           // rows, columns, steps, strides
+constexpr int64_t kMaxExtent = (int64_t)1 << 40;  // values between a matrix's first and last
+
+bool type_ok(int t) { return t == QL_F32 || t == QL_F16 || t == QL_BF16; }
+size_t type_size(int t) { return t == QL_F32 ? 4 : 2; }
+bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+// Whether m rows of `cols` values with leading dimension ld can be addressed.
+bool rows_ok(int64_t ld, int64_t m, int64_t cols) {
+  return ld >= cols && ld <= kMaxDim && m * ld <= kMaxExtent;
+}
+// Whether two matrices of m rows (leading dimensions lda, ldb >= cols) share
+// values other than by being one and the same (`same` returns that).  Column
+// slices of one buffer do not.
+bool rows_clash(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t m, int64_t cols,
+                size_t e, bool *same = nullptr) {
+  if (same) *same = false;
+  if (!a || !b || m <= 0 || cols <= 0) return false;
+  if (a == b && (lda == ldb || m == 1)) {
+    if (same) *same = true;
+    return false;
+  }
+  if (!share_bytes(a, (size_t)((m - 1) * lda + cols) * e, b, (size_t)((m - 1) * ldb + cols) * e))
+    return false;
+  if (lda != ldb || m == 1) return true;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  const uintptr_t pitch = (uintptr_t)lda * e, w = (uintptr_t)cols * e;
+  const uintptr_t r = y > x ? (y - x) % pitch : (pitch - (x - y) % pitch) % pitch;
+  return r < w || pitch - r < w;
+}
+
+// Rows (t, b) of a sequence: strides that can be addressed; of an output, rows
+// that do not overlap.
+bool seq_ok(const ql_seq &q, int64_t T, int64_t B, int64_t D, bool output) {
+  if (q.t_stride < 0 || q.b_stride < 0 || q.t_stride > kMaxExtent || q.b_stride > kMaxExtent)
+    return false;
+  if (T <= 0 || B <= 0) return true;
+  // (T and B are below 2^21 and 2^16, so the products stay within 64 bits)
+  const int64_t t = (T - 1) * q.t_stride, b = (B - 1) * q.b_stride;
+  if (t + b + D > kMaxExtent) return false;
+  if (!output) return true;
+  if (T > 1 && q.t_stride < D) return false;
+  if (B > 1 && q.b_stride < D) return false;
+  return T == 1 || B == 1 || q.t_stride >= b + D || q.b_stride >= t + D;
+}
+// Whether sequence a (rows of wa values) shares values with b (rows of wb) other
+// than by being one and the same (`same` returns that).
+bool seq_clash(const ql_seq &a, int64_t wa, const ql_seq &b, int64_t wb, int64_t T, int64_t B,
+               size_t e, bool *same) {
+  *same = false;
+  if (!a.data || !b.data || T <= 0 || B <= 0) return false;
+  const bool alike = (T == 1 || a.t_stride == b.t_stride) && (B == 1 || a.b_stride == b.b_stride);
+  if (a.data == b.data && alike && wa == wb) {
+    *same = true;
+    return false;
+  }
+  auto bytes = [&](const ql_seq &q, int64_t w) {
+    return (size_t)((T - 1) * q.t_stride + (B - 1) * q.b_stride + w) * e;
+  };
+  if (!share_bytes(a.data, bytes(a, wa), b.data, bytes(b, wb))) return false;
+  if (!alike) return true;
+  // rows at multiples of one pitch: the offset between the two within it decides
+  const int64_t st = T > 1 ? a.t_stride : 0, sb = B > 1 ? a.b_stride : 0;
+  const int64_t pitch = st && sb ? std::min(st, sb) : st ? st : sb;
+  if (pitch == 0 || (st && st % pitch) || (sb && sb % pitch)) return true;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.data), y = reinterpret_cast<uintptr_t>(b.data);
+  const uintptr_t p = (uintptr_t)pitch * e;
+  const uintptr_t r = y > x ? (y - x) % p : (p - (x - y) % p) % p;
+  return r < (uintptr_t)wa * e || p - r < (uintptr_t)wb * e;
+}
+
+// A state read and written: apart, or one buffer.
+bool state_clash(const float *in, const float *out, size_t bytes) {
+  return in != out && share_bytes(in, bytes, out, bytes);
+}
+
+ql_status check_qmatrix4(const ql_qmatrix4 *q) {
+  if (!q || !q->codes || !q->zero || !q->inv_q) return QL_EINVAL;
+  if (q->rows < 0 || q->cols <= 0 || q->rows > kMaxDim || q->cols > kMaxDim - 127) return QL_ESHAPE;
+  if (q->group != 32 && q->group != 64 && q->group != 128) return QL_EUNSUPPORTED;
+  if (q->ld != round_up(q->cols, 128)) return QL_ESHAPE;
+  if (!aligned(q->codes, 16) || !aligned(q->inv_q, 16) || !aligned(q->zero, 4)) return QL_EINVAL;
+  return QL_OK;
+}
+Q4Mat weight4(const ql_qmatrix4 &q) {
+  return Q4Mat{q.codes, q.rows, q.ld, q.group, round_up(q.rows, 16), q.zero, q.inv_q};
+}
+// Blocks of 64 rows of X per launch.
+bool matmul4_rows_ok(int64_t m) { return m <= (int64_t)65535 * 64; }
+
+SeqIn seq_in(const ql_seq *q) {
+  return q ? SeqIn{q->data, q->t_stride, q->b_stride} : SeqIn{nullptr, 0, 0};
+}
+constexpr int64_t kMaxSteps = (int64_t)1 << 20, kMaxSequences = 65535;
+
+}  // namespace
+
+ql_status ql_rms_norm(ql_type type, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                      const float *weight, int64_t m, int64_t cols, double eps, void *sum,
+                      int64_t lds, void *y, int64_t ldy, const ql_qact *codes, float *rstd,
+                      void *stream) {
+  const int t = enum_arg(type);
+  if (!type_ok(t)) return QL_EINVAL;
+  if (!(eps >= 0.0) || std::isinf(eps)) return QL_EINVAL;
+  if (!sum && !y && !codes && !rstd) return QL_EINVAL;
+  if (m < 0 || cols <= 0 || m > kMaxDim || cols > kMaxDim - 63) return QL_ESHAPE;
+  if (!rows_ok(ldx, m, cols) || (residual && !rows_ok(ldr, m, cols)) ||
+      (sum && !rows_ok(lds, m, cols)) || (y && !rows_ok(ldy, m, cols)))
+    return QL_ESHAPE;
+  if (codes && (codes->rows != m || codes->cols != cols || codes->ld % 64 != 0 ||
+                !rows_ok(codes->ld, m, cols)))
+    return QL_ESHAPE;
+  if (m == 0) return QL_OK;
+  if (!x) return QL_EINVAL;
+  const size_t e = type_size(t);
+  bool same = false;
+  if (rows_clash(x, ldx, sum, lds, m, cols, e) || rows_clash(x, ldx, y, ldy, m, cols, e) ||
+      rows_clash(residual, ldr, sum, lds, m, cols, e) ||
+      rows_clash(residual, ldr, y, ldy, m, cols, e) ||
+      rows_clash(sum, lds, y, ldy, m, cols, e, &same) || same)
+    return QL_EINVAL;
+  NormArgs a{};
+  if (codes) {
+    if (!codes->codes || !codes->zero || !codes->inv_q || !codes->sums) return QL_EINVAL;
+    auto on_codes = [&](const void *p, int64_t ld) {
+      return share_bytes(codes->codes, (size_t)(m * codes->ld), p,
+                         (size_t)((m - 1) * ld + cols) * e);
+    };
+    if (on_codes(x, ldx) || on_codes(residual, ldr) || on_codes(sum, lds) || on_codes(y, ldy))
+      return QL_EINVAL;
+    a.codes = codes->codes;
+    a.ldc = codes->ld;
+    a.zero = codes->zero;
+    a.inv_q = codes->inv_q;
+    a.sums = codes->sums;
+  }
+  a.rows = m;
+  a.cols = cols;
+  a.x = x;
+  a.ldx = ldx;
+  a.residual = residual;
+  a.ldr = ldr;
+  a.weight = weight;
+  a.eps = eps;
+  a.sum = sum;
+  a.lds = lds;
+  a.y = y;
+  a.ldy = ldy;
+  a.rstd = rstd;
+  return from_hip(launch_rms_norm(t, a, as_stream(stream)));
+}
+
+size_t ql_rms_norm_backward_workspace(int64_t m, int64_t cols) {
+  if (m < 0 || cols <= 0 || m > kMaxDim || cols > kMaxDim) return 0;
+  return rms_norm_backward_ws(m, cols);
+}
+
+ql_status ql_rms_norm_backward(ql_type type, const void *dy, int64_t lddy, const void *v,
+                               int64_t ldv, const float *rstd, const float *weight,
+                               const void *dsum, int64_t ldds, int64_t m, int64_t cols, void *dx,
+                               int64_t lddx, float *dweight, void *ws, size_t ws_bytes,
+                               void *stream) {
+  const int t = enum_arg(type);
+  if (!type_ok(t)) return QL_EINVAL;
+  if (m < 0 || cols <= 0 || m > kMaxDim || cols > kMaxDim - 63) return QL_ESHAPE;
+  if (!rows_ok(lddy, m, cols) || !rows_ok(ldv, m, cols) || !rows_ok(lddx, m, cols) ||
+      (dsum && !rows_ok(ldds, m, cols)))
+    return QL_ESHAPE;
+  if (m > 0 && (!dy || !v || !rstd || !dx)) return QL_EINVAL;
+  const size_t e = type_size(t);
+  if (rows_clash(dy, lddy, dx, lddx, m, cols, e) || rows_clash(v, ldv, dx, lddx, m, cols, e) ||
+      rows_clash(dsum, ldds, dx, lddx, m, cols, e))
+    return QL_EINVAL;
+  if (dweight && (!ws || ws_bytes < rms_norm_backward_ws(m, cols))) return QL_EWORKSPACE;
+  if (m == 0 && !dweight) return QL_OK;
+  NormGradArgs a{};
+  a.rows = m;
+  a.cols = cols;
+  a.dy = dy;
+  a.lddy = lddy;
+  a.v = v;
+  a.ldv = ldv;
+  a.dsum = dsum;
+  a.ldds = ldds;
+  a.rstd = rstd;
+  a.weight = weight;
+  a.dx = dx;
+  a.lddx = lddx;
+  a.dweight = dweight;
+  return from_hip(launch_rms_norm_backward(t, a, static_cast<float *>(ws), as_stream(stream)));
+}
+
+ql_status ql_quantize4(const float *src, int64_t rows, int64_t cols, ql_qmatrix4 *dst,
+                       void *stream) {
+  ql_status st = check_qmatrix4(dst);
+  if (st != QL_OK) return st;
+  if (dst->rows != rows || dst->cols != cols) return QL_ESHAPE;
+  if (rows > 0 && !src) return QL_EINVAL;
+  return from_hip(launch_quantize4(src, weight4(*dst), cols, as_stream(stream)));
+}
+
+ql_status ql_dequantize4(const ql_qmatrix4 *q, float *dst, void *stream) {
+  ql_status st = check_qmatrix4(q);
+  if (st != QL_OK) return st;
+  if (q->rows > 0 && !dst) return QL_EINVAL;
+  return from_hip(launch_dequantize4(weight4(*q), q->cols, dst, as_stream(stream)));
+}
+
+ql_status ql_matmul4(const ql_qmatrix4 *W, const ql_qact *X, const float *bias, ql_type type,
+                     void *Y, void *stream) {
+  ql_status st = check_qmatrix4(W);
+  if (st != QL_OK) return st;
+  const int t = enum_arg(type);
+  if (!X || !type_ok(t)) return QL_EINVAL;
+  const int64_t m = X->rows;
+  if (m < 0 || X->cols != W->cols || X->ld % 64 != 0 || !rows_ok(X->ld, m, X->cols))
+    return QL_ESHAPE;
+  if (!matmul4_rows_ok(m)) return QL_EUNSUPPORTED;
+  if (m == 0 || W->rows == 0) return QL_OK;
+  if (!X->codes || !X->zero || !X->inv_q || !Y || !aligned(X->codes, 16)) return QL_EINVAL;
+  if (share_bytes(X->codes, (size_t)(m * X->ld), Y, (size_t)(m * W->rows) * type_size(t)))
+    return QL_EINVAL;
+  return from_hip(launch_matmul4(weight4(*W), ActRows{X->codes, X->ld, X->zero, X->inv_q, X->sums},
+                                 m, bias, t, Y, as_stream(stream)));
+}
+
+size_t ql_quantized_matmul4_workspace(int64_t m, int64_t cols) {
+  if (m < 0 || cols <= 0 || m > kMaxDim || cols > kMaxDim - 63) return 0;
+  Carve c(nullptr);
+  take_act(c, m, cols);
+  return c.off;
+}
+
+ql_status ql_quantized_matmul4(const ql_qmatrix4 *W, ql_type xtype, const void *X, int64_t ldx,
+                               int64_t m, const float *bias, ql_type ytype, void *Y, void *ws,
+                               size_t ws_bytes, void *stream) {
+  ql_status st = check_qmatrix4(W);
+  if (st != QL_OK) return st;
+  const int tx = enum_arg(xtype), ty = enum_arg(ytype);
+  if (!type_ok(tx) || !type_ok(ty)) return QL_EINVAL;
+  if (m < 0 || !rows_ok(ldx, m, W->cols)) return QL_ESHAPE;
+  if (!matmul4_rows_ok(m)) return QL_EUNSUPPORTED;
+  if (m == 0 || W->rows == 0) return QL_OK;
+  if (!X || !Y) return QL_EINVAL;
+  if (!ws || ws_bytes < ql_quantized_matmul4_workspace(m, W->cols)) return QL_EWORKSPACE;
+  hipStream_t s = as_stream(stream);
+  Carve c(ws);
+  const ActBuf x = take_act(c, m, W->cols);
+  if (launch_quantize_rows_of(tx, X, ldx, m, W->cols, x.codes, x.ld, x.zero, x.inv_q, x.sums, s) !=
+      hipSuccess)
+    return QL_EHIP;
+  return from_hip(launch_matmul4(weight4(*W), x.rows(), m, bias, ty, Y, s));
+}
+
+ql_status ql_causal_conv(ql_type type, const ql_seq *x, const float *w, const float *bias,
+                         int32_t width, int32_t silu, int64_t T, int64_t B, int64_t D,
+                         const int32_t *lengths, const float *state_in, float *state_out,
+                         const ql_seq *y, void *stream) {
+  const int t = enum_arg(type);
+  if (!type_ok(t) || !x || !y || !w || (silu != 0 && silu != 1)) return QL_EINVAL;
+  if (T < 0 || B < 0 || D <= 0 || D > kMaxDim || width < 1) return QL_ESHAPE;
+  if (width > 8 || T > kMaxSteps || B > kMaxSequences) return QL_EUNSUPPORTED;
+  if (!seq_ok(*x, T, B, D, false) || !seq_ok(*y, T, B, D, true)) return QL_ESHAPE;
+  if (T * B > 0 && (!x->data || !y->data)) return QL_EINVAL;
+  bool same = false;
+  if (seq_clash(*x, D, *y, D, T, B, type_size(t), &same) || same) return QL_EINVAL;
+  if (state_clash(state_in, state_out, (size_t)(B * (width - 1) * D) * 4)) return QL_EINVAL;
+  ConvArgs a{};
+  a.T = T;
+  a.B = B;
+  a.D = D;
+  a.x = seq_in(x);
+  a.w = w;
+  a.bias = bias;
+  a.silu = silu;
+  a.lengths = lengths;
+  a.state_in = state_in;
+  a.state_out = state_out;
+  a.y = const_cast<void *>(y->data);
+  a.y_t = y->t_stride;
+  a.y_b = y->b_stride;
+  return from_hip(launch_causal_conv(t, a, width, as_stream(stream)));
+}
+
+size_t ql_selective_scan_workspace(int64_t channels, int64_t states, int64_t T, int64_t B) {
+  if (channels <= 0 || channels > kMaxDim || states < 1 || states > 64 || T < 0 || T > kMaxSteps ||
+      B < 0 || B > kMaxSequences)
+    return 0;
+  return scan_ws(channels, states, T, B);
+}
+
+ql_status ql_selective_scan(ql_type type, const ql_scan *P, const ql_seq *u, const ql_seq *delta,
+                            const ql_seq *Bm, const ql_seq *Cm, const ql_seq *z, int64_t T,
+                            int64_t B, const int32_t *lengths, const float *state_in,
+                            float *state_out, const ql_seq *y, void *ws, size_t ws_bytes,
+                            void *stream) {
+  const int t = enum_arg(type);
+  if (!type_ok(t) || !P || !P->A || !u || !delta || !Bm || !Cm || !y) return QL_EINVAL;
+  if (P->softplus != 0 && P->softplus != 1) return QL_EINVAL;
+  const int64_t D = P->channels, N = P->states;
+  if (T < 0 || B < 0 || D <= 0 || D > kMaxDim || N < 1) return QL_ESHAPE;
+  if (N > 64 || T > kMaxSteps || B > kMaxSequences) return QL_EUNSUPPORTED;
+  if (!seq_ok(*u, T, B, D, false) || !seq_ok(*delta, T, B, D, false) ||
+      !seq_ok(*Bm, T, B, N, false) || !seq_ok(*Cm, T, B, N, false) ||
+      (z && !seq_ok(*z, T, B, D, false)) || !seq_ok(*y, T, B, D, true))
+    return QL_ESHAPE;
+  if (T * B > 0 && (!u->data || !delta->data || !Bm->data || !Cm->data || !y->data))
+    return QL_EINVAL;
+  const size_t e = type_size(t);
+  bool same = false;
+  if (seq_clash(*u, D, *y, D, T, B, e, &same) || seq_clash(*delta, D, *y, D, T, B, e, &same) ||
+      (z && seq_clash(*z, D, *y, D, T, B, e, &same)) ||
+      seq_clash(*Bm, N, *y, D, T, B, e, &same) || same ||
+      seq_clash(*Cm, N, *y, D, T, B, e, &same) || same)
+    return QL_EINVAL;
+  if (state_clash(state_in, state_out, (size_t)(B * N * D) * 4)) return QL_EINVAL;
+  const size_t need = scan_ws(D, N, T, B);
+  if (need > 0 && (!ws || ws_bytes < need)) return QL_EWORKSPACE;
+  ScanArgs a{};
+  a.T = T;
+  a.B = B;
+  a.D = D;
+  a.N = (int)N;
+  a.u = seq_in(u);
+  a.delta = seq_in(delta);
+  a.Bm = seq_in(Bm);
+  a.Cm = seq_in(Cm);
+  a.z = seq_in(z);
+  a.A = P->A;
+  a.skip = P->D;
+  a.delta_bias = P->delta_bias;
+  a.softplus = P->softplus;
+  a.lengths = lengths;
+  a.state_in = state_in;
+  a.state_out = state_out;
+  a.y = const_cast<void *>(y->data);
+  a.y_t = y->t_stride;
+  a.y_b = y->b_stride;
+  return from_hip(launch_scan(t, a, ws, as_stream(stream)));
+}
+
 }  // extern "C"

@@ -311,4 +311,82 @@ size_t xbptt_ws(int64_t B);
 hipError_t launch_xbptt(const BpttArgs &a, int cus, int lds_max, hipStream_t s, bool *done);
 int xbptt_launches(int64_t H, int64_t T, int64_t B, int cus, int lds_max);
 
+// ---- root-mean-square norm (ql_norm.hip); type: ql_type (0 fp32, 1 fp16, 2 bfloat16)
+struct NormArgs {
+  int64_t rows, cols;
+  const void *x, *residual;  // residual nullable
+  int64_t ldx, ldr;
+  const float *weight;       // nullable: ones
+  double eps;
+  void *sum, *y;             // nullable
+  int64_t lds, ldy;
+  int8_t *codes;             // nullable, with the per-row arrays below
+  int64_t ldc;
+  int32_t *zero, *sums;
+  float *inv_q;
+  float *rstd;               // nullable
+};
+hipError_t launch_rms_norm(int type, const NormArgs &a, hipStream_t s);
+struct NormGradArgs {
+  int64_t rows, cols;
+  const void *dy, *v, *dsum;  // dsum nullable
+  int64_t lddy, ldv, ldds;
+  const float *rstd, *weight; // weight nullable: ones
+  void *dx;
+  int64_t lddx;
+  float *dweight;             // nullable
+};
+size_t rms_norm_backward_ws(int64_t rows, int64_t cols);
+hipError_t launch_rms_norm_backward(int type, const NormGradArgs &a, float *part, hipStream_t s);
+
+// ---- 4-bit weights with group scales (ql_q4.hip)
+struct Q4Mat {
+  uint8_t *codes;      // [rows][ld / 2]
+  int64_t rows, ld;    // ld: columns up to a multiple of 128
+  int group;           // 32, 64 or 128
+  int64_t ldr;         // rows up to a multiple of 16
+  int8_t *zero;        // [ld / group][ldr]
+  float *inv_q;        // [ld / group][ldr]
+};
+hipError_t launch_quantize4(const float *W, const Q4Mat &q, int64_t cols, hipStream_t s);
+hipError_t launch_dequantize4(const Q4Mat &q, int64_t cols, float *dst, hipStream_t s);
+hipError_t launch_quantize_rows_of(int type, const void *X, int64_t ldx, int64_t m, int64_t K,
+                                   int8_t *codes, int64_t ld, int32_t *zero, float *inv_q,
+                                   int32_t *sums, hipStream_t s);
+hipError_t launch_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, int ytype,
+                          void *Y, hipStream_t s);
+
+// ---- causal convolution and selective scan (ql_ssm.hip)
+struct SeqIn {
+  const void *data;
+  int64_t t_stride, b_stride;  // elements; channels contiguous
+};
+struct ConvArgs {
+  int64_t T, B, D;
+  SeqIn x;
+  const float *w, *bias;       // [W][D]; [D], nullable
+  int silu;
+  const int32_t *lengths;      // [B], nullable
+  const float *state_in;       // [B][W - 1][D], nullable: zeros
+  float *state_out;            // nullable
+  void *y;
+  int64_t y_t, y_b;
+};
+hipError_t launch_causal_conv(int type, const ConvArgs &a, int width, hipStream_t s);
+struct ScanArgs {
+  int64_t T, B, D;
+  int N;
+  SeqIn u, delta, Bm, Cm, z;   // z.data nullable
+  const float *A;              // [N][D]
+  const float *skip, *delta_bias;  // [D], nullable
+  int softplus;
+  const int32_t *lengths;      // [B], nullable
+  const float *state_in;       // [B][N][D], nullable: zeros
+  float *state_out;            // nullable
+  void *y;
+  int64_t y_t, y_b;
+};
+size_t scan_ws(int64_t D, int64_t N, int64_t T, int64_t B);
+hipError_t launch_scan(int type, const ScanArgs &a, void *ws, hipStream_t s);
+
 }  // namespace ql

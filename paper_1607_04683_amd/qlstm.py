@@ -37,8 +37,13 @@ EXPORTS = [
     "ql_acoustic_model_forward_frames", "ql_acoustic_model_forward_stream",
     "ql_acoustic_model_forward_stream_noalloc", "ql_train_step_workspace", "ql_train_step",
     "ql_debug_set_wait_bound", "ql_debug_recurrence_layout", "ql_debug_stack_layout",
-    "ql_debug_model_layout", "ql_debug_float_layout",
+    "ql_debug_model_layout", "ql_debug_float_layout", "ql_rms_norm",
+    "ql_rms_norm_backward_workspace", "ql_rms_norm_backward", "ql_quantize4", "ql_dequantize4",
+    "ql_matmul4", "ql_quantized_matmul4_workspace", "ql_quantized_matmul4", "ql_causal_conv",
+    "ql_selective_scan_workspace", "ql_selective_scan",
 ]
+QL_F32, QL_F16, QL_BF16 = 0, 1, 2
+QL_TYPES = {torch.float32: QL_F32, torch.float16: QL_F16, torch.bfloat16: QL_BF16}
 
 
 class QLError(RuntimeError):
@@ -97,6 +102,21 @@ class CTrainLayer(C.Structure):
 class CTrainModel(C.Structure):
     _fields_ = [("nlayers", C.c_int32), ("layers", C.POINTER(CTrainLayer)), ("states", C.c_int64),
                 ("Wy", C.c_void_p), ("by", C.c_void_p)]
+
+
+class CQMatrix4(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("ld", C.c_int64), ("group", C.c_int32), ("zero", C.c_void_p),
+                ("inv_q", C.c_void_p)]
+
+
+class CSeq(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("t_stride", C.c_int64), ("b_stride", C.c_int64)]
+
+
+class CScan(C.Structure):
+    _fields_ = [("channels", C.c_int64), ("states", C.c_int64), ("A", C.c_void_p),
+                ("D", C.c_void_p), ("delta_bias", C.c_void_p), ("softplus", C.c_int32)]
 
 
 class CModelTaps(C.Structure):
@@ -184,6 +204,28 @@ def load(path: str = LIB_PATH):
     L.ql_f32_acoustic_model_workspace.restype = sz
     L.ql_f32_acoustic_model_forward.argtypes = [C.POINTER(CF32Model), vp, i64, i64, vp, vp, sz,
                                                 vp]
+    dbl, seq = C.c_double, C.POINTER(CSeq)
+    L.ql_rms_norm.argtypes = [i32, vp, i64, vp, i64, vp, i64, i64, dbl, vp, i64, vp, i64,
+                              C.POINTER(CQAct), vp, vp]
+    L.ql_rms_norm_backward_workspace.argtypes = [i64, i64]
+    L.ql_rms_norm_backward_workspace.restype = sz
+    L.ql_rms_norm_backward.argtypes = [i32, vp, i64, vp, i64, vp, vp, vp, i64, i64, i64, vp, i64,
+                                       vp, vp, sz, vp]
+    L.ql_quantize4.argtypes = [vp, i64, i64, C.POINTER(CQMatrix4), vp]
+    L.ql_dequantize4.argtypes = [C.POINTER(CQMatrix4), vp, vp]
+    L.ql_matmul4.argtypes = [C.POINTER(CQMatrix4), C.POINTER(CQAct), vp, i32, vp, vp]
+    L.ql_quantized_matmul4_workspace.argtypes = [i64, i64]
+    L.ql_quantized_matmul4_workspace.restype = sz
+    L.ql_quantized_matmul4.argtypes = [C.POINTER(CQMatrix4), i32, vp, i64, i64, vp, i32, vp, vp, sz,
+                                       vp]
+    L.ql_causal_conv.argtypes = [i32, seq, vp, vp, i32, i32, i64, i64, i64, vp, vp, vp, seq, vp]
+    L.ql_selective_scan_workspace.argtypes = [i64, i64, i64, i64]
+    L.ql_selective_scan_workspace.restype = sz
+    L.ql_selective_scan.argtypes = [i32, C.POINTER(CScan), seq, seq, seq, seq, seq, i64, i64, vp,
+                                    vp, vp, seq, vp, sz, vp]
+    for f in ("ql_rms_norm", "ql_rms_norm_backward", "ql_quantize4", "ql_dequantize4",
+              "ql_matmul4", "ql_quantized_matmul4", "ql_causal_conv", "ql_selective_scan"):
+        getattr(L, f).restype = i32
     for f in ("ql_quantize", "ql_dequantize", "ql_quantized_matmul", "ql_gemm_u8",
               "ql_lstm_layer_forward", "ql_acoustic_model_forward", "ql_workspace_status",
               "ql_gate_fn", "ql_lstm_recurrence", "ql_f32_matmul", "ql_f32_lstm_layer_forward",
@@ -858,3 +900,334 @@ def float_layout(H: int, T: int, B: int, backward: bool = False) -> int:
     """Launches in which the fp32 recurrence (or the training step's backward one)
     runs with a part of the batch on each XCD; 0: as tiles over the chip."""
     return int(load().ql_debug_float_layout(int(backward), H, T, B))
+
+
+# --------------------------------------------- a quantized state-space block
+def _need(t, name, shape, dtype=torch.float32, device=None):
+    """A dense parameter or buffer of the given shape, type and device -> its address."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: {dtype} {tuple(shape)} wanted, got {t.dtype} {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} lies on {t.device}, the other tensors on {device}")
+    return t.data_ptr()
+
+
+def _here(t, name):
+    """The device of t, which must be the current one: calls run on its current stream."""
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must lie on the current GPU, got {t.device}")
+    return t.device
+
+
+def _rows(t, name, like=None):
+    """A matrix with contiguous rows -> (address, leading dimension)."""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or t.dtype not in QL_TYPES:
+        raise ValueError(f"{name}: rows of fp32, fp16 or bfloat16 wanted")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype
+                             or t.device != like.device):
+        raise ValueError(f"{name}: {like.dtype} {tuple(like.shape)} on {like.device} wanted, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    m, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the values of a row must be contiguous")
+    return t.data_ptr(), t.stride(0) if m > 1 else cols
+
+
+def rms_norm(x: torch.Tensor, weight=None, residual=None, eps: float = 1e-6, want=("y",),
+             out: dict | None = None) -> dict:
+    """ql_rms_norm on rows x [m][cols] -> dict of what `want` names: "y" and "sum"
+    (x + residual) of x's type, "codes" (QAct), "rstd" fp32 [m].  out: buffers to use."""
+    dev = _here(x, "x")
+    px, ldx = _rows(x, "x")
+    pr, ldr = _rows(residual, "residual", x)
+    m, cols = x.shape
+    res = {}
+    for k in want:
+        t = out.get(k) if out else None
+        if t is None:
+            if k == "codes":
+                t = QAct(torch.empty(m, ld_for(cols), dtype=torch.int8, device=dev), cols,
+                         torch.empty(m, dtype=torch.int32, device=dev),
+                         torch.empty(m, dtype=torch.float32, device=dev),
+                         torch.empty(m, dtype=torch.int32, device=dev))
+            elif k == "rstd":
+                t = torch.empty(m, dtype=torch.float32, device=dev)
+            elif k in ("y", "sum"):
+                t = torch.empty(m, cols, dtype=x.dtype, device=dev)
+            else:
+                raise ValueError(f"want: y, sum, codes and rstd are known, not {k!r}")
+        res[k] = t
+    q, y, s, rstd = res.get("codes"), res.get("y"), res.get("sum"), res.get("rstd")
+    ps, lds = _rows(s, "sum", x)
+    py, ldy = _rows(y, "y", x)
+    cq = None
+    if q is not None:
+        _check_qact(q, m, cols, dev)
+        cq = C.byref(q.cstruct())
+    _check(load().ql_rms_norm(QL_TYPES[x.dtype], px, ldx, pr, ldr,
+                              _need(weight, "weight", (cols,), device=dev), m, cols, eps, ps, lds,
+                              py, ldy, cq, _need(rstd, "rstd", (m,), device=dev), _stream()),
+           "ql_rms_norm")
+    return res
+
+
+def _check_qact(q: QAct, m: int, cols: int, dev, sums: bool = True):
+    if q.cols != cols or q.codes.dim() != 2 or q.codes.shape[0] != m:
+        raise ValueError(f"codes: {m} rows of {cols} columns wanted")
+    _need(q.codes, "codes", q.codes.shape, torch.int8, dev)
+    _need(q.zero, "codes' zero points", (m,), torch.int32, dev)
+    _need(q.inv_q, "codes' recovery factors", (m,), torch.float32, dev)
+    if sums:
+        _need(q.sums, "codes' sums", (m,), torch.int32, dev)
+
+
+def dequantize_activations(q: QAct) -> torch.Tensor:
+    """Recovered rows [m][cols] fp32 of per-vector codes (ql_dequantize, a row a block)."""
+    dev = _here(q.codes, "codes")
+    m = q.codes.shape[0]
+    _check_qact(q, m, q.cols, dev, sums=False)
+    out = torch.empty(m, q.cols, dtype=torch.float32, device=dev)
+    if m == 0:
+        return out
+    cs = CQMatrix(q.codes.data_ptr(), m, q.cols, q.codes.shape[1], m, None, q.zero.data_ptr(),
+                  q.inv_q.data_ptr(), None)
+    _check(load().ql_dequantize(C.byref(cs), out.data_ptr(), _stream()), "ql_dequantize")
+    return out
+
+
+def rms_norm_backward(dy: torch.Tensor, v: torch.Tensor, rstd: torch.Tensor, weight=None, dsum=None,
+                      want_dweight: bool = True, out: dict | None = None,
+                      workspace: Workspace | None = None):
+    """ql_rms_norm_backward -> (dx of dy's type, dweight fp32 [cols] or None).  v: the
+    rows that were normed (x, or sum with a residual).  out: buffers "dx", "dweight"."""
+    dev = _here(dy, "dy")
+    m, cols = dy.shape
+    pdy, lddy = _rows(dy, "dy")
+    pv, ldv = _rows(v, "v", dy)
+    pds, ldds = _rows(dsum, "dsum", dy)
+    o = out or {}
+    dx = o.get("dx")
+    if dx is None:
+        dx = torch.empty(m, cols, dtype=dy.dtype, device=dev)
+    dw = o.get("dweight")
+    if dw is None and want_dweight:
+        dw = torch.empty(cols, dtype=torch.float32, device=dev)
+    pdx, lddx = _rows(dx, "dx", dy)
+    lib = load()
+    ws = None
+    if dw is not None:
+        ws = (workspace or Workspace()).get(lib.ql_rms_norm_backward_workspace(m, cols), dev)
+    _check(lib.ql_rms_norm_backward(QL_TYPES[dy.dtype], pdy, lddy, pv, ldv,
+                                    _need(rstd, "rstd", (m,), device=dev),
+                                    _need(weight, "weight", (cols,), device=dev), pds, ldds, m,
+                                    cols, pdx, lddx, _need(dw, "dweight", (cols,), device=dev),
+                                    None if ws is None else ws.data_ptr(),
+                                    0 if ws is None else ws.numel(), _stream()),
+           "ql_rms_norm_backward")
+    return dx, dw
+
+
+@dataclass
+class QMatrix4:
+    """A matrix in 4 bits with a scale and a zero point per group of columns (see
+    ql_qmatrix4 for the layout)."""
+    codes: torch.Tensor   # uint8 [rows][ld / 2]
+    rows: int
+    cols: int
+    group: int
+    zero: torch.Tensor    # int8 [ld / group][rows up to a multiple of 16]
+    inv_q: torch.Tensor   # float32, the same
+
+    @property
+    def ld(self) -> int:
+        return 2 * self.codes.shape[1]
+
+    def cstruct(self) -> CQMatrix4:
+        c, z, q = self.codes, self.zero, self.inv_q
+        ld = 2 * c.shape[1]
+        dims = (ld // self.group if self.group else 0, (self.rows + 15) // 16 * 16)
+        if c.shape[0] != self.rows or z.shape != dims or q.shape != dims:
+            raise ValueError(f"QMatrix4: arrays of other shapes than {self.rows} x {self.cols} in "
+                             f"groups of {self.group} has")
+        if c.dtype != torch.uint8 or z.dtype != torch.int8 or q.dtype != torch.float32:
+            raise ValueError("QMatrix4: uint8 codes, int8 zero and float32 inv_q wanted")
+        if not (c.is_contiguous() and z.is_contiguous() and q.is_contiguous()):
+            raise ValueError("QMatrix4: arrays must be contiguous")
+        if not c.device == z.device == q.device:
+            raise ValueError("QMatrix4: arrays on different devices")
+        return CQMatrix4(c.data_ptr(), self.rows, self.cols, ld, self.group, z.data_ptr(),
+                         q.data_ptr())
+
+    @staticmethod
+    def empty(rows: int, cols: int, group: int, device) -> "QMatrix4":
+        ld, ldr = (cols + 127) // 128 * 128, (rows + 15) // 16 * 16
+        n = ld // group
+        return QMatrix4(torch.empty(rows, ld // 2, dtype=torch.uint8, device=device), rows, cols,
+                        group, torch.zeros(n, ldr, dtype=torch.int8, device=device),
+                        torch.zeros(n, ldr, dtype=torch.float32, device=device))
+
+    @staticmethod
+    def of_codes(codes: torch.Tensor, zero: torch.Tensor, inv_q: torch.Tensor,
+                 group: int) -> "QMatrix4":
+        """A matrix quantized elsewhere: codes 0..15 [rows][cols], and per row and group
+        (the last may be partial) the zero point in -15..0 and the recovery factor:
+        value (code + zero) inv_q."""
+        rows, cols = codes.shape
+        q = QMatrix4.empty(rows, cols, group, codes.device)
+        n = -(-cols // group)
+        if zero.shape != (rows, n) or inv_q.shape != (rows, n):
+            raise ValueError(f"zero and inv_q: [{rows}][{n}] wanted")
+        if rows and (int(codes.max()) > 15 or int(codes.min()) < 0 or int(zero.max()) > 0
+                     or int(zero.min()) < -15):
+            raise ValueError("codes lie in 0..15, zero points in -15..0")
+        q.zero[:n, :rows] = zero.t().to(torch.int8)
+        q.inv_q[:n, :rows] = inv_q.t()
+        # what is padded recovers to 0
+        full = (-q.zero[:, :rows].t()).to(torch.uint8).repeat_interleave(group, 1)
+        full[:, :cols] = codes.to(torch.uint8)
+        c = (full ^ 8).reshape(rows, -1, 4, 4, 2, 4).permute(0, 1, 3, 2, 4, 5)
+        q.codes.copy_((c[..., 0, :] | (c[..., 1, :] << 4)).reshape(rows, -1))
+        return q
+
+    def codes_u8(self) -> torch.Tensor:
+        """V' (0..15) as uint8 [rows][cols]."""
+        w = self.codes.reshape(self.rows, -1, 4, 4, 1, 4)
+        c = (torch.cat([w & 15, w >> 4], 4) ^ 8).permute(0, 1, 3, 2, 4, 5)
+        return c.reshape(self.rows, self.ld)[:, :self.cols]
+
+
+def quantize4(W: torch.Tensor, group: int = 64) -> QMatrix4:
+    """W [rows][cols] fp32 (device) -> QMatrix4, groups of 32, 64 or 128 columns."""
+    dev = _here(W, "W")
+    if W.dim() != 2 or W.dtype != torch.float32:
+        raise ValueError("W: an fp32 matrix wanted")
+    if group not in (32, 64, 128):
+        raise ValueError("group: 32, 64 or 128")
+    W = W.contiguous()
+    rows, cols = W.shape
+    q = QMatrix4.empty(rows, cols, group, dev)
+    cs = q.cstruct()
+    _check(load().ql_quantize4(W.data_ptr(), rows, cols, C.byref(cs), _stream()), "ql_quantize4")
+    return q
+
+
+def dequantize4(q: QMatrix4) -> torch.Tensor:
+    dev = _here(q.codes, "codes")
+    out = torch.empty(q.rows, q.cols, dtype=torch.float32, device=dev)
+    cs = q.cstruct()
+    _check(load().ql_dequantize4(C.byref(cs), out.data_ptr(), _stream()), "ql_dequantize4")
+    return out
+
+
+def matmul4(q: QMatrix4, x, bias=None, out_dtype=None, out: torch.Tensor | None = None,
+            workspace: Workspace | None = None) -> torch.Tensor:
+    """Y [m][rows] = recovered x times recovered q^T (+ bias): x a QAct
+    (ql_matmul4), or rows [m][cols] of fp32, fp16 or bfloat16, quantized on the fly
+    (ql_quantized_matmul4).  Y of out_dtype; by default x's type, fp32 for codes."""
+    lib = load()
+    cs = q.cstruct()
+    dev = _here(q.codes, "the matrix")
+    act = isinstance(x, QAct)
+    if act:
+        m = x.codes.shape[0]
+        _check_qact(x, m, q.cols, dev, sums=False)
+        dt = out_dtype or torch.float32
+    else:
+        px, ldx = _rows(x, "x")
+        m = x.shape[0]
+        if x.shape[1] != q.cols or x.device != dev:
+            raise ValueError(f"x: rows of {q.cols} columns on {dev} wanted")
+        dt = out_dtype or x.dtype
+    if dt not in QL_TYPES:
+        raise ValueError(f"out_dtype: fp32, fp16 or bfloat16 wanted, got {dt}")
+    if out is None:
+        out = torch.empty(m, q.rows, dtype=dt, device=dev)
+    py, pb = _need(out, "out", (m, q.rows), dt, dev), _need(bias, "bias", (q.rows,), device=dev)
+    if act:
+        cx = x.cstruct()
+        _check(lib.ql_matmul4(C.byref(cs), C.byref(cx), pb, QL_TYPES[dt], py, _stream()),
+               "ql_matmul4")
+    else:
+        ws = (workspace or Workspace()).get(lib.ql_quantized_matmul4_workspace(m, q.cols), dev)
+        _check(lib.ql_quantized_matmul4(C.byref(cs), QL_TYPES[x.dtype], px, ldx, m, pb,
+                                        QL_TYPES[dt], py, ws.data_ptr(), ws.numel(), _stream()),
+               "ql_quantized_matmul4")
+    return out
+
+
+def _seq(t, name, T, B, width, dtype, dev):
+    if t is None:
+        return None
+    if t.shape != (T, B, width) or t.dtype != dtype or t.device != dev:
+        raise ValueError(f"{name}: {dtype} [{T}][{B}][{width}] on {dev} wanted, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    st, sb, sc = t.stride()
+    if width > 1 and sc != 1:
+        raise ValueError(f"{name}: the channels of a step must be contiguous")
+    return CSeq(t.data_ptr(), st if T > 1 else 0, sb if B > 1 else 0)
+
+
+def causal_conv(x: torch.Tensor, weight: torch.Tensor, bias=None, silu: bool = True, lengths=None,
+                state_in=None, state_out=None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """ql_causal_conv: x [T][B][D] (any strides over T and B), weight [width][D], bias [D];
+    states [B][width - 1][D] fp32 -> y of x's type and shape.  Rows of a sequence past
+    its length are left as they are in `out` (undefined in a new tensor)."""
+    dev = _here(x, "x")
+    if x.dim() != 3 or x.dtype not in QL_TYPES or weight.dim() != 2:
+        raise ValueError("x: [T][B][D] of fp32, fp16 or bfloat16, and weight [width][D] wanted")
+    T, B, D = x.shape
+    W = weight.shape[0]
+    cx = _seq(x, "x", T, B, D, x.dtype, dev)
+    if out is None:
+        out = torch.empty(T, B, D, dtype=x.dtype, device=dev)
+    cy = _seq(out, "out", T, B, D, x.dtype, dev)
+    state = (B, W - 1, D)
+    _check(load().ql_causal_conv(QL_TYPES[x.dtype], cx, _need(weight, "weight", (W, D), device=dev),
+                                 _need(bias, "bias", (D,), device=dev), W, int(bool(silu)), T, B, D,
+                                 _need(lengths, "lengths", (B,), torch.int32, dev),
+                                 _need(state_in, "state_in", state, device=dev),
+                                 _need(state_out, "state_out", state, device=dev), cy, _stream()),
+           "ql_causal_conv")
+    return out
+
+
+def selective_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, Bm: torch.Tensor,
+                   Cm: torch.Tensor, D=None, z=None, delta_bias=None, softplus: bool = True,
+                   lengths=None, state_in=None, state_out=None, out: torch.Tensor | None = None,
+                   workspace: Workspace | None = None) -> torch.Tensor:
+    """ql_selective_scan: u, delta and z [T][B][channels], Bm and Cm [T][B][states] of one
+    type (any strides over T and B), A [states][channels], D and delta_bias [channels] fp32,
+    states [B][states][channels] fp32 -> y of u's type.  Rows of a sequence past its
+    length are left as they are in `out` (undefined in a new tensor)."""
+    dev = _here(u, "u")
+    if u.dim() != 3 or u.dtype not in QL_TYPES or A.dim() != 2:
+        raise ValueError("u: [T][B][channels] of fp32, fp16 or bfloat16, and A [states][channels] "
+                         "wanted")
+    T, B, ch = u.shape
+    N, dt = A.shape[0], u.dtype
+    if out is None:
+        out = torch.empty(T, B, ch, dtype=dt, device=dev)
+    P = CScan(ch, N, _need(A, "A", (N, ch), device=dev), _need(D, "D", (ch,), device=dev),
+              _need(delta_bias, "delta_bias", (ch,), device=dev), int(bool(softplus)))
+    lib = load()
+    nbytes = lib.ql_selective_scan_workspace(ch, N, T, B)
+    ws = (workspace or Workspace()).get(nbytes, dev) if nbytes else None
+    state = (B, N, ch)
+    _check(lib.ql_selective_scan(QL_TYPES[dt], P, _seq(u, "u", T, B, ch, dt, dev),
+                                 _seq(delta, "delta", T, B, ch, dt, dev),
+                                 _seq(Bm, "Bm", T, B, N, dt, dev), _seq(Cm, "Cm", T, B, N, dt, dev),
+                                 _seq(z, "z", T, B, ch, dt, dev), T, B,
+                                 _need(lengths, "lengths", (B,), torch.int32, dev),
+                                 _need(state_in, "state_in", state, device=dev),
+                                 _need(state_out, "state_out", state, device=dev),
+                                 _seq(out, "out", T, B, ch, dt, dev),
+                                 None if ws is None else ws.data_ptr(),
+                                 0 if ws is None else ws.numel(), _stream()),
+           "ql_selective_scan")
+    return out

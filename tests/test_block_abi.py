@@ -1,0 +1,215 @@
+"""What the calls of a quantized state-space block refuse, without a GPU: every
+call below fails (or has nothing to do) before the library touches memory or
+the HIP runtime."""
+import ctypes as C
+import os
+
+import numpy as np
+import pytest
+import torch
+
+import block_reference as ref
+
+P = 1 << 32  # never dereferenced
+
+
+@pytest.fixture(scope="module")
+def ql():
+    from paper_1607_04683_amd import qlstm
+    if not os.path.exists(qlstm.LIB_PATH):
+        from paper_1607_04683_amd import build
+        build.build(force=False)
+    return qlstm
+
+
+def at(elements, size=4):
+    return P + elements * size
+
+
+def test_rms_norm_refusals(ql):
+    lib = ql.load()
+
+    def call(type=0, x=P, ldx=100, r=None, ldr=0, m=8, n=100, eps=1e-6, sum=None, lds=0, y=2 * P,
+             ldy=100, codes=None, rstd=None):
+        return lib.ql_rms_norm(type, x, ldx, r, ldr, None, m, n, eps, sum, lds, y, ldy,
+                               None if codes is None else C.byref(codes), rstd, None)
+
+    assert call(m=0) == ql.QL_OK and call(m=0, x=None) == ql.QL_OK
+    assert call(type=3) == call(type=-1) == ql.QL_EINVAL
+    for eps in (-1e-9, float("nan"), float("inf")):
+        assert call(eps=eps) == ql.QL_EINVAL
+    assert call(x=None) == ql.QL_EINVAL
+    assert call(y=None) == ql.QL_EINVAL                              # no result wanted
+    assert call(m=-1) == call(n=0) == call(n=-5) == ql.QL_ESHAPE
+    assert call(ldx=99) == call(ldy=99) == ql.QL_ESHAPE
+    assert call(r=3 * P, ldr=99) == call(sum=3 * P, lds=99) == ql.QL_ESHAPE
+    assert call(m=1 << 31) == call(m=1 << 30, ldx=1 << 30, n=100) == ql.QL_ESHAPE
+    # results on inputs: exactly or not at all
+    assert call(y=at(4)) == ql.QL_EINVAL
+    assert call(y=P, ldy=101) == ql.QL_EINVAL                        # another spacing
+    assert call(sum=at(100), lds=100) == ql.QL_EINVAL                # a row later
+    assert call(r=3 * P, ldr=100, sum=3 * P + 4, lds=100) == ql.QL_EINVAL
+    assert call(sum=2 * P, lds=100) == ql.QL_EINVAL                  # sum is y
+    assert call(ldx=300, y=at(250), ldy=300, n=100) == ql.QL_EINVAL  # slices that wrap into the next row
+    good = ql.CQAct(3 * P, 8, 100, 128, P, P, P)
+    bad = lambda **k: ql.CQAct(*[k.get(n, getattr(good, n)) for n, _ in good._fields_])
+    assert call(codes=bad(rows=7)) == call(codes=bad(cols=99)) == ql.QL_ESHAPE
+    assert call(codes=bad(ld=64)) == call(codes=bad(ld=100)) == ql.QL_ESHAPE
+    for f in ("codes", "zero", "inv_q", "sums"):
+        assert call(codes=bad(**{f: None})) == ql.QL_EINVAL
+    assert call(codes=bad(codes=P + 64)) == call(codes=bad(codes=2 * P - 64)) == ql.QL_EINVAL
+
+
+def test_rms_norm_backward_refusals(ql):
+    lib = ql.load()
+    need = lib.ql_rms_norm_backward_workspace(8, 100)
+    assert need > 0
+    assert lib.ql_rms_norm_backward_workspace(-1, 100) == lib.ql_rms_norm_backward_workspace(8, 0) == 0
+
+    def call(type=0, dy=P, lddy=100, v=2 * P, ldv=100, rstd=P, ds=None, ldds=0, m=8, n=100, dx=3 * P,
+             lddx=100, dw=P, ws=P, wsb=need):
+        return lib.ql_rms_norm_backward(type, dy, lddy, v, ldv, rstd, None, ds, ldds, m, n, dx, lddx, dw,
+                                        ws, wsb, None)
+
+    assert call(type=3) == ql.QL_EINVAL
+    assert call(dy=None) == call(v=None) == call(rstd=None) == call(dx=None) == ql.QL_EINVAL
+    assert call(m=-1) == call(n=0) == ql.QL_ESHAPE
+    assert call(lddy=99) == call(ldv=99) == call(lddx=99) == call(ds=P, ldds=99) == ql.QL_ESHAPE
+    assert call(ws=None) == call(wsb=need - 1) == ql.QL_EWORKSPACE
+    assert call(dx=at(3)) == call(dx=2 * P + 400) == ql.QL_EINVAL
+    assert call(ds=4 * P, ldds=100, dx=4 * P + 4) == ql.QL_EINVAL
+    assert call(m=0, dw=None, ws=None) == ql.QL_OK
+
+
+def q4(ql, **k):
+    d = dict(codes=P, rows=8, cols=100, ld=128, group=64, zero=P, inv_q=P)
+    d.update(k)
+    return ql.CQMatrix4(*[d[n] for n, _ in ql.CQMatrix4._fields_])
+
+
+def test_4bit_refusals(ql):
+    lib = ql.load()
+    x = lambda **k: ql.CQAct(*[k.get(n, v) for n, v in (("codes", 2 * P), ("rows", 4), ("cols", 100),
+                                                        ("ld", 128), ("zero", P), ("inv_q", P),
+                                                        ("sums", None))])
+    mm = lambda w, a=x(), t=0, Y=3 * P: lib.ql_matmul4(
+        None if w is None else C.byref(w), None if a is None else C.byref(a), None, t, Y, None)
+    need = lib.ql_quantized_matmul4_workspace(4, 100)
+    assert need >= 4 * 128 + 3 * 16
+    assert lib.ql_quantized_matmul4_workspace(-1, 100) == lib.ql_quantized_matmul4_workspace(4, 0) == 0
+    qm = lambda w=q4(ql), tx=0, X=2 * P, ldx=100, m=4, ty=0, Y=3 * P, ws=P, wsb=need: \
+        lib.ql_quantized_matmul4(C.byref(w), tx, X, ldx, m, None, ty, Y, ws, wsb, None)
+    calls = [mm, lambda w: qm(w), lambda w: lib.ql_quantize4(P, 8, 100, C.byref(w), None),
+             lambda w: lib.ql_dequantize4(C.byref(w), 3 * P, None)]
+    for call in calls:
+        for f in ("codes", "zero", "inv_q"):
+            assert call(q4(ql, **{f: None})) == ql.QL_EINVAL
+        assert call(q4(ql, group=16)) == call(q4(ql, group=96)) == call(q4(ql, group=0)) == ql.QL_EUNSUPPORTED
+        assert call(q4(ql, ld=64)) == call(q4(ql, ld=256)) == call(q4(ql, cols=0, ld=0)) == ql.QL_ESHAPE
+        assert call(q4(ql, rows=-1)) == ql.QL_ESHAPE
+        assert call(q4(ql, codes=P + 8)) == call(q4(ql, inv_q=P + 4)) == call(q4(ql, zero=P + 2)) == ql.QL_EINVAL
+    assert mm(None) == mm(q4(ql), None) == ql.QL_EINVAL
+    assert mm(q4(ql), t=5) == mm(q4(ql), Y=None) == mm(q4(ql), x(codes=None)) == ql.QL_EINVAL
+    assert mm(q4(ql), x(zero=None)) == mm(q4(ql), x(inv_q=None)) == mm(q4(ql), x(codes=2 * P + 8)) == ql.QL_EINVAL
+    assert mm(q4(ql), x(cols=99)) == mm(q4(ql), x(ld=64)) == mm(q4(ql), x(ld=100)) == ql.QL_ESHAPE
+    assert mm(q4(ql), x(rows=-1)) == ql.QL_ESHAPE
+    assert mm(q4(ql), x(rows=4194241)) == ql.QL_EUNSUPPORTED
+    assert mm(q4(ql), Y=2 * P + 100) == ql.QL_EINVAL                  # Y on the codes
+    assert mm(q4(ql), x(rows=0)) == mm(q4(ql, rows=0)) == ql.QL_OK
+    assert lib.ql_quantize4(P, 7, 100, C.byref(q4(ql)), None) == ql.QL_ESHAPE
+    assert lib.ql_quantize4(None, 8, 100, C.byref(q4(ql)), None) == ql.QL_EINVAL
+    assert lib.ql_dequantize4(C.byref(q4(ql)), None, None) == ql.QL_EINVAL
+    assert qm(tx=3) == qm(ty=3) == qm(X=None) == qm(Y=None) == ql.QL_EINVAL
+    assert qm(ldx=99) == qm(m=-1) == ql.QL_ESHAPE
+    assert qm(ws=None) == qm(wsb=need - 1) == ql.QL_EWORKSPACE
+    assert qm(m=0) == ql.QL_OK
+
+
+def seq(ql, data, t=200, b=100):
+    return ql.CSeq(data, t, b)
+
+
+def test_causal_conv_refusals(ql):
+    lib = ql.load()
+
+    def call(type=0, x=seq(ql, P), w=P, width=4, silu=1, T=5, B=2, D=100, si=None, so=None,
+             y=seq(ql, 2 * P)):
+        return lib.ql_causal_conv(type, x, w, None, width, silu, T, B, D, None, si, so, y, None)
+
+    assert call(B=0) == ql.QL_OK
+    assert call(type=3) == call(x=None) == call(y=None) == call(w=None) == call(silu=2) == ql.QL_EINVAL
+    assert call(x=seq(ql, None)) == call(y=seq(ql, None)) == ql.QL_EINVAL
+    assert call(T=-1) == call(B=-1) == call(D=0) == call(width=0) == ql.QL_ESHAPE
+    assert call(width=9) == call(T=(1 << 20) + 1) == call(B=65536) == ql.QL_EUNSUPPORTED
+    assert call(x=seq(ql, P, -1)) == call(x=seq(ql, P, 200, -1)) == ql.QL_ESHAPE
+    # rows of y on each other
+    assert call(y=seq(ql, 2 * P, 99)) == call(y=seq(ql, 2 * P, 200, 99)) == ql.QL_ESHAPE
+    assert call(y=seq(ql, 2 * P, 150, 100)) == call(y=seq(ql, 2 * P, 0, 100)) == ql.QL_ESHAPE
+    assert call(y=seq(ql, P)) == call(y=seq(ql, P + 4)) == ql.QL_EINVAL  # y on x
+    assert call(si=P, so=P + 4) == ql.QL_EINVAL                          # states that overlap in part
+
+
+def test_selective_scan_refusals(ql):
+    lib = ql.load()
+    T, B, D, N = 5, 2, 100, 16
+    need = lib.ql_selective_scan_workspace(D, N, T, B)
+    assert lib.ql_selective_scan_workspace(0, N, T, B) == lib.ql_selective_scan_workspace(D, 65, T, B) == 0
+
+    def call(type=0, p=True, ch=D, n=N, A=P, softplus=1, u=seq(ql, P), dl=seq(ql, 2 * P),
+             Bm=seq(ql, 3 * P, 32, 16), Cm=seq(ql, 4 * P, 32, 16), z=seq(ql, 5 * P), T=T, B=B, si=None,
+             so=None, y=seq(ql, 6 * P), ws=P, wsb=1 << 40):
+        c = ql.CScan(ch, n, A, None, None, softplus)
+        return lib.ql_selective_scan(type, c if p else None, u, dl, Bm, Cm, z, T, B, None, si, so, y, ws,
+                                     wsb, None)
+
+    assert call(B=0) == ql.QL_OK
+    assert call(type=3) == call(p=False) == call(A=None) == call(softplus=2) == ql.QL_EINVAL
+    for k in ("u", "dl", "Bm", "Cm", "y"):
+        assert call(**{k: None}) == ql.QL_EINVAL
+        assert call(**{k: seq(ql, None)}) == ql.QL_EINVAL
+    assert call(T=-1) == call(B=-1) == call(ch=0) == call(n=0) == ql.QL_ESHAPE
+    assert call(n=65) == call(T=(1 << 20) + 1) == call(B=65536) == ql.QL_EUNSUPPORTED
+    for k in ("u", "dl", "Bm", "Cm", "z"):
+        assert call(**{k: seq(ql, 7 * P, -1)}) == ql.QL_ESHAPE
+    assert call(y=seq(ql, 6 * P, 99)) == call(y=seq(ql, 6 * P, 150)) == ql.QL_ESHAPE
+    # y near u, delta, z, B or C, but not exactly on the first three
+    for base in (P, 2 * P, 5 * P):
+        assert call(y=seq(ql, base + 4)) == ql.QL_EINVAL
+    assert call(y=seq(ql, 3 * P)) == call(y=seq(ql, 4 * P - 400)) == ql.QL_EINVAL
+    assert call(si=P, so=P + 4) == ql.QL_EINVAL
+    if need:
+        assert call(ws=None) == call(wsb=need - 1) == ql.QL_EWORKSPACE
+
+
+def test_binding_refusals(ql):
+    """The binding checks types, shapes and the device before it calls the library."""
+    x = torch.zeros(4, 64)
+    for f in (lambda: ql.rms_norm(x), lambda: ql.rms_norm_backward(x, x, torch.zeros(4)),
+              lambda: ql.quantize4(x), lambda: ql.causal_conv(x[None], torch.zeros(4, 64)),
+              lambda: ql.matmul4(ql.QMatrix4.empty(8, 64, 64, "cpu"), x),
+              lambda: ql.selective_scan(x[None], x[None], x, x[None], x[None])):
+        with pytest.raises(ValueError, match="current GPU"):
+            f()
+    q = ql.QMatrix4.empty(8, 64, 64, "cpu")
+    for bad in (dict(rows=9), dict(group=32), dict(group=0), dict(zero=q.zero.int()), dict(inv_q=q.inv_q.t())):
+        with pytest.raises(ValueError):
+            ql.QMatrix4(**{**q.__dict__, **bad}).cstruct()
+    with pytest.raises(ValueError):
+        ql.QMatrix4.of_codes(torch.full((2, 64), 16), torch.zeros(2, 1), torch.ones(2, 1), 64)
+
+
+@pytest.mark.parametrize("rows,cols,group", [(1, 1, 32), (3, 130, 64), (17, 256, 128), (5, 33, 32)])
+def test_4bit_layout(ql, rows, cols, group):
+    """of_codes and codes_u8 are each other's inverse, and the layout is the documented one."""
+    W = torch.randn(rows, cols, generator=torch.Generator().manual_seed(cols))
+    codes, zero, inv_q = ref.quantize4(W.double().numpy(), group)
+    q = ql.QMatrix4.of_codes(*(torch.from_numpy(a) for a in (codes, zero, inv_q)), group)
+    assert np.array_equal(q.codes_u8().numpy(), codes)
+    words = q.codes.numpy().view("<u4").reshape(rows, -1)
+    for k in range(q.ld):
+        run, at_ = divmod(k, 128)
+        p, i, j = at_ // 32, at_ % 32 // 8, at_ % 8
+        half = (words[:, 16 * run + 4 * i + p] >> (8 * j if j < 4 else 8 * (j - 4) + 4)) & 15
+        signed = (half.astype(int) ^ 8) - 8
+        want = codes[:, k].astype(int) if k < cols else -q.zero.numpy()[k // group, :rows].astype(int)
+        assert np.array_equal(signed + 8, want)

@@ -1,0 +1,541 @@
+"""The operators of a quantized state-space block on the GPU against their
+definitions in 64 bits: the norm with the residual's addition (its 8-bit codes
+bit for bit), its backward pass, 4-bit weights and their products, the causal
+convolution and the selective scan.  Tolerances come from block_reference's
+bounds: counted roundings, not measured differences."""
+import numpy as np
+import pytest
+import torch
+
+import block_reference as ref
+from block_reference import TYPES, f64
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def ql():
+    assert torch.cuda.is_available(), "GPU tests need an MI355X"
+    from paper_1607_04683_amd import qlstm
+    qlstm.load()
+    return qlstm
+
+
+def gen(seed):
+    g = torch.Generator().manual_seed(seed)
+    return lambda *s: torch.randn(*s, generator=g)
+
+
+def ident(p):
+    return str(p).replace("torch.", "")
+
+
+# ------------------------------------------------------------------------ norm
+def norm_values(x, residual, weight, rstd):
+    """v and the fp32 y of the definition, from the GPU's own rstd (CPU, fp32)."""
+    v = x if residual is None else (x.float() + residual.float()).to(x.dtype)
+    y = v.float() * rstd[:, None]
+    return v, y if weight is None else y * weight
+
+
+def check_norm(r, x, residual, weight, eps):
+    v, _ = norm_values(x, residual, weight, torch.ones(x.shape[0]))
+    want = 1 / np.sqrt((f64(v) ** 2).sum(1) / x.shape[1] + eps)
+    rstd = r["rstd"].cpu()
+    # rounded once from fp64
+    assert (np.abs(f64(rstd) - want) <= want * ref.U32 * (1 + 1e-6)).all()
+    v, y = norm_values(x, residual, weight, rstd)
+    if "sum" in r:
+        assert torch.equal(r["sum"].cpu(), v)
+    if "y" in r:
+        assert torch.equal(r["y"].cpu(), y.to(x.dtype))
+    if "codes" in r:
+        q = r["codes"]
+        codes, zero, inv_q = ref.quantize8(f64(y))
+        n = x.shape[1]
+        got = q.codes.cpu()
+        assert np.array_equal(got[:, :n].numpy().view(np.uint8) ^ 0x80, codes)
+        assert not got[:, n:].any()
+        assert np.array_equal(q.zero.cpu().numpy(), zero)
+        assert np.array_equal(q.inv_q.cpu().numpy(), inv_q)
+        assert np.array_equal(q.sums.cpu().numpy(), codes.astype(np.int64).sum(1))
+
+
+NORM_SHAPES = [(1, 1), (3, 5), (2, 64), (5, 320), (9, 500), (4, 1023), (3, 2048), (6, 1000), (300, 130),
+               (2, 4096), (2, 8192), (2, 8193), (1, 20011), (3, 16384), (257, 72)]
+
+
+@pytest.mark.parametrize("m,n", NORM_SHAPES)
+@pytest.mark.parametrize("dtype", TYPES, ids=ident)
+@pytest.mark.parametrize("residual", [False, True])
+def test_norm(ql, m, n, dtype, residual):
+    z = gen(m * 31 + n)
+    x, w = z(m, n).to(dtype), 1 + 0.2 * z(n)
+    r = (3 * z(m, n)).to(dtype) if residual else None
+    got = ql.rms_norm(x.to(DEV), w.to(DEV), residual=None if r is None else r.to(DEV), eps=1e-5,
+                      want=("y", "sum", "codes", "rstd"))
+    check_norm(got, x, r, w, 1e-5)
+
+
+@pytest.mark.parametrize("want", [("y",), ("codes",), ("sum",), ("rstd",), ("sum", "codes"), ("y", "rstd")])
+@pytest.mark.parametrize("n", [500, 20000])
+def test_norm_single_results_and_no_weight(ql, want, n):
+    z = gen(5)
+    x, r = z(7, n), z(7, n)
+    got = ql.rms_norm(x.to(DEV), residual=r.to(DEV), eps=0.0, want=want)
+    assert set(got) == set(want)
+    if "rstd" not in got:
+        got["rstd"] = ql.rms_norm(x.to(DEV), residual=r.to(DEV), eps=0.0, want=("rstd",))["rstd"]
+    check_norm(got, x, r, None, 0.0)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ident)
+@pytest.mark.parametrize("m,n,ld,at", [(6, 500, 1003, 1), (5, 512, 1536, 512), (4, 130, 131, 0),
+                                       (3, 9000, 18001, 7)])
+def test_norm_column_slices_in_place_and_around(ql, dtype, m, n, ld, at):
+    """Slices of wider buffers, off any alignment; sum on the residual and y on x; the
+    columns around the results stay as they are."""
+    z = gen(n + ld)
+    bx, br, w = z(m, ld).to(dtype), z(m, ld).to(dtype), 1 + 0.1 * z(n)
+    gx, gr = bx.to(DEV), br.to(DEV)
+    x, r = bx[:, at:at + n].clone(), br[:, at:at + n].clone()
+    sx, sr = gx[:, at:at + n], gr[:, at:at + n]
+    got = ql.rms_norm(sx, w.to(DEV), residual=sr, want=("y", "sum", "codes", "rstd"),
+                      out=dict(y=sx, sum=sr))
+    check_norm(got, x, r, w, 1e-6)
+    keep = torch.ones(ld, dtype=torch.bool)
+    keep[at:at + n] = False
+    assert torch.equal(gx.cpu()[:, keep], bx[:, keep]) and torch.equal(gr.cpu()[:, keep], br[:, keep])
+    # the other way round: y on the residual, sum on x
+    gx, gr = bx.to(DEV), br.to(DEV)
+    sx, sr = gx[:, at:at + n], gr[:, at:at + n]
+    got = ql.rms_norm(sx, w.to(DEV), residual=sr, want=("y", "sum", "rstd"), out=dict(y=sr, sum=sx))
+    check_norm(got, x, r, w, 1e-6)
+    # y on x without sum
+    gx, gr = bx.to(DEV), br.to(DEV)
+    sx, sr = gx[:, at:at + n], gr[:, at:at + n]
+    got = ql.rms_norm(sx, w.to(DEV), residual=sr, want=("y", "codes", "rstd"), out=dict(y=sx))
+    check_norm(got, x, r, w, 1e-6)
+
+
+def test_norm_codes_equal_the_quantizer_on_y(ql):
+    z = gen(11)
+    x, w = (z(37, 700) * torch.logspace(-20, 20, 37)[:, None]).to(DEV), (1 + z(700)).to(DEV)
+    r = ql.rms_norm(x, w, want=("y", "codes"))
+    q = ql.quantize_activations(r["y"])
+    for a, b in ((r["codes"].codes, q.codes), (r["codes"].zero, q.zero), (r["codes"].inv_q, q.inv_q),
+                 (r["codes"].sums, q.sums)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n", [96, 5000, 17000])
+@pytest.mark.parametrize("dtype", TYPES, ids=ident)
+def test_norm_rows_that_are_not_finite_or_zero(ql, n, dtype):
+    z = gen(3)
+    x = z(6, n).to(dtype)
+    x[1] = 0
+    x[2, n // 2] = float("nan")
+    x[3, n - 1] = float("inf")
+    x[4, 0] = float("-inf")
+    w = torch.ones(n)
+    r = ql.rms_norm(x.to(DEV), w.to(DEV), want=("y", "codes", "rstd"))
+    y, q = r["y"].cpu(), r["codes"]
+    assert torch.isnan(y[2]).all() and torch.isnan(y[3, n - 1]) and (y[1] == 0).all()
+    bad = torch.tensor([False, False, True, True, True, False])
+    assert torch.equal(torch.isnan(q.inv_q.cpu()), bad)
+    assert not q.zero.cpu()[bad].any() and not q.sums.cpu()[bad].any()
+    good = ~bad
+    sel = lambda t: t[good.to(t.device)]
+    check_norm(dict(y=sel(r["y"]), rstd=sel(r["rstd"]),
+                    codes=ql.QAct(sel(q.codes), n, sel(q.zero), sel(q.inv_q), sel(q.sums))),
+               x[good], None, w, 1e-6)
+    # one weight that is not finite: every row's codes say so
+    w[n // 3] = float("nan")
+    q = ql.rms_norm(x.to(DEV), w.to(DEV), want=("codes",))["codes"]
+    assert torch.isnan(q.inv_q).all()
+    # eps = 0 on a row of zeros: 0 / 0
+    r = ql.rms_norm(torch.zeros(1, n, dtype=dtype, device=DEV), eps=0.0, want=("y", "codes"))
+    assert torch.isnan(r["y"]).all() and torch.isnan(r["codes"].inv_q).all()
+
+
+def test_norm_no_rows(ql):
+    r = ql.rms_norm(torch.empty(0, 64, device=DEV), want=("y", "sum", "codes", "rstd"))
+    assert r["y"].shape == (0, 64) and r["codes"].codes.shape == (0, 64)
+
+
+GRAD_SHAPES = [(1, 1), (3, 5), (5, 320), (70, 500), (33, 1023), (40, 2048), (300, 130), (17, 4096),
+               (5, 8193), (2, 20011), (1000, 64), (129, 1000)]
+
+
+@pytest.mark.parametrize("m,n", GRAD_SHAPES)
+@pytest.mark.parametrize("dtype", TYPES, ids=ident)
+@pytest.mark.parametrize("dsum", [False, True])
+def test_norm_backward(ql, m, n, dtype, dsum):
+    z = gen(m * 17 + n)
+    v, dy, w = z(m, n).to(dtype), z(m, n).to(dtype), 1 + 0.2 * z(n)
+    ds = z(m, n).to(dtype) if dsum else None
+    rstd = torch.rsqrt(v.double().square().mean(1) + 1e-6).float()
+    dx, dw = ql.rms_norm_backward(dy.to(DEV), v.to(DEV), rstd.to(DEV), w.to(DEV),
+                                  dsum=None if ds is None else ds.to(DEV))
+    want = ref.rms_norm_backward(f64(dy), f64(v), f64(rstd), f64(w), None if ds is None else f64(ds), n)
+    ref.close(dx, want[0], want[1], dtype, "dx")
+    ref.close(dw, want[2], want[3], torch.float32, "dweight")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ident)
+@pytest.mark.parametrize("m,n,ld,at", [(6, 500, 1003, 1), (40, 512, 1536, 512), (3, 9000, 18001, 7)])
+def test_norm_backward_slices_and_in_place(ql, dtype, m, n, ld, at):
+    z = gen(n + ld)
+    bufs = [z(m, ld).to(dtype) for _ in range(3)]
+    w = 1 + 0.1 * z(n)
+    dy, v, ds = (b[:, at:at + n].clone() for b in bufs)
+    rstd = torch.rsqrt(v.double().square().mean(1) + 1e-6).float()
+    want = ref.rms_norm_backward(f64(dy), f64(v), f64(rstd), f64(w), f64(ds), n)
+    for k in range(3):
+        g = [b.to(DEV) for b in bufs]
+        s = [b[:, at:at + n] for b in g]
+        dx, dw = ql.rms_norm_backward(s[0], s[1], rstd.to(DEV), w.to(DEV), dsum=s[2], out=dict(dx=s[k]))
+        ref.close(dx, want[0], want[1], dtype, "dx")
+        ref.close(dw, want[2], want[3], torch.float32, "dweight")
+        keep = torch.ones(ld, dtype=torch.bool)
+        keep[at:at + n] = False
+        assert torch.equal(g[k].cpu()[:, keep], bufs[k][:, keep])
+
+
+def test_norm_backward_no_weight_no_dweight_no_rows(ql):
+    z = gen(2)
+    v, dy = z(5, 70), z(5, 70)
+    rstd = torch.rsqrt(v.double().square().mean(1)).float()
+    dx, dw = ql.rms_norm_backward(dy.to(DEV), v.to(DEV), rstd.to(DEV), want_dweight=False)
+    assert dw is None
+    want = ref.rms_norm_backward(f64(dy), f64(v), f64(rstd), np.ones(70), None, 70)
+    ref.close(dx, want[0], want[1], torch.float32, "dx")
+    e = torch.empty(0, 70, device=DEV)
+    dx, dw = ql.rms_norm_backward(e, e, torch.empty(0, device=DEV), torch.ones(70, device=DEV))
+    assert dx.shape == (0, 70) and not dw.any()
+
+
+def test_norm_backward_against_differences(ql):
+    """The directional derivative of sum(dy y) of the forward kernel.  The quotient's
+    own error: the rounding of y (3 half steps an element), and the truncation,
+    which the formula in 64 bits has alike."""
+    z = gen(8)
+    m, n, h, eps = 4, 96, 2.0 ** -7, 1e-3
+    v, dy, w, d, dwd = z(m, n), z(m, n), 1 + 0.2 * z(n), z(m, n), z(n)
+
+    def loss64(v_, w_):
+        y = f64(v_) / np.sqrt((f64(v_) ** 2).mean(1, keepdims=True) + eps) * f64(w_)
+        return (f64(dy) * y).sum()
+
+    def loss(v_, w_):
+        y = ql.rms_norm(v_.to(DEV), w_.to(DEV), eps=eps)["y"]
+        return (f64(dy) * f64(y)).sum()
+
+    up, dn = v + h * d, v - h * d   # as fp32 holds them
+    wu, wd = w + h * dwd, w - h * dwd
+    rstd = ql.rms_norm(v.to(DEV), eps=eps, want=("rstd",))["rstd"]
+    dx, dw = ql.rms_norm_backward(dy.to(DEV), v.to(DEV), rstd, w.to(DEV))
+    y64 = np.abs(f64(v) / np.sqrt((f64(v) ** 2).mean(1, keepdims=True) + eps) * f64(w))
+    noise = (np.abs(f64(dy)) * y64).sum() * 1.2 * 4 * ref.U32 / h
+    for got, q, q64 in (((f64(dx) * f64(d)).sum(), (loss(up, w) - loss(dn, w)) / (2 * h),
+                         (loss64(up, w) - loss64(dn, w)) / (2 * h)),
+                        ((f64(dw) * f64(dwd)).sum(), (loss(v, wu) - loss(v, wd)) / (2 * h),
+                         (loss64(v, wu) - loss64(v, wd)) / (2 * h))):
+        assert abs(q - q64) <= noise
+        # truncation: the same quotient at half the step is four times nearer
+    r64 = 1 / np.sqrt((f64(v) ** 2).mean(1) + eps)
+    e = ref.rms_norm_backward(f64(dy), f64(v), r64, f64(w), None, n)
+    for got, want, bound, a, b in ((dx, e[0], e[1], (up, w), (dn, w)), (dw, e[2], e[3], (v, wu), (v, wd))):
+        dirn = f64(d) if got is dx else f64(dwd)
+        q = (loss(*a) - loss(*b)) / (2 * h)
+        q64 = (loss64(*a) - loss64(*b)) / (2 * h)
+        trunc = abs(q64 - (want * dirn).sum())
+        slack = noise + trunc + (bound * np.abs(dirn)).sum() + 4 * ref.U32 * np.abs(want * dirn).sum()
+        assert abs((f64(got) * dirn).sum() - q) <= slack
+
+
+# ---------------------------------------------------------------- 4-bit weights
+Q4_SHAPES = [(1, 1), (3, 31), (16, 32), (17, 33), (5, 127), (33, 128), (64, 129), (100, 500), (7, 1000),
+             (257, 320), (2, 4097)]
+
+
+@pytest.mark.parametrize("rows,cols", Q4_SHAPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_quantize4(ql, rows, cols, group):
+    z = gen(rows + cols + group)
+    W = 0.05 * z(rows, cols)
+    if rows > 4:
+        W[1], W[2], W[3, : cols // 2], W[4] = 0, W[2].abs() + 1, 0, -W[4].abs()
+    q = ql.quantize4(W.to(DEV), group)
+    codes, zero, inv_q = ref.quantize4(f64(W), group)
+    n = zero.shape[1]
+    assert np.array_equal(q.codes_u8().cpu().numpy(), codes)
+    assert np.array_equal(q.zero[:n, :rows].t().cpu().numpy(), zero)
+    assert np.array_equal(q.inv_q[:n, :rows].t().cpu().numpy(), inv_q)
+    back = (codes.astype(np.float32) + np.repeat(zero, group, 1)[:, :cols]) * np.repeat(inv_q, group, 1)[:, :cols]
+    assert np.array_equal(ql.dequantize4(q).cpu().numpy(), back)
+    # padded columns recover to 0
+    whole = ql.QMatrix4(q.codes, rows, q.ld, group, q.zero, q.inv_q)
+    assert not ql.dequantize4(whole)[:, cols:].any()
+    # the same matrix from codes made elsewhere
+    p = ql.QMatrix4.of_codes(torch.from_numpy(codes).to(DEV), torch.from_numpy(zero).to(DEV),
+                             torch.from_numpy(inv_q).to(DEV), group)
+    assert torch.equal(p.codes, q.codes) and torch.equal(ql.dequantize4(p), ql.dequantize4(q))
+
+
+def qact(ql, X):
+    """Rows quantized by the framework, and the same on the CPU."""
+    codes, zero, inv_q = ref.quantize8(f64(X))
+    q = ql.quantize_activations(X.to(DEV))
+    assert np.array_equal(q.codes.cpu().numpy()[:, : X.shape[1]].view(np.uint8) ^ 0x80, codes)
+    return q, codes, zero, inv_q
+
+
+MM_SHAPES = [(1, 1, 1), (1, 16, 32), (1, 100, 500), (2, 33, 129), (3, 2000, 500), (15, 17, 127),
+             (16, 64, 64), (17, 31, 200), (33, 100, 1000), (64, 257, 128), (65, 48, 320), (130, 20, 96),
+             (6, 5, 4097), (1, 300, 8192), (48, 130, 2048), (200, 70, 257), (1, 4000, 64), (4, 8192, 130)]
+
+
+@pytest.mark.parametrize("m,rows,cols", MM_SHAPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype", TYPES, ids=ident)
+def test_matmul4(ql, m, rows, cols, group, dtype):
+    z = gen(m + rows + cols)
+    W, X, b = 0.05 * z(rows, cols), z(m, cols), 0.1 * z(rows)
+    q = ql.quantize4(W.to(DEV), group)
+    codes, zero, inv_q = ref.quantize4(f64(W), group)
+    # codes in, fp32 or narrower out, with a bias
+    x, xc, xz, xq = qact(ql, X)
+    Y, bound = ref.matmul4(codes, zero, inv_q, group, xc, xz, xq)
+    ref.close(ql.matmul4(q, x, b.to(DEV), out_dtype=dtype), Y + f64(b),
+              bound + 2 * ref.U32 * (np.abs(Y) + np.abs(f64(b))), dtype, "codes")
+    # rows of each type in, without a bias
+    Xt = X.to(dtype)
+    xc, xz, xq = ref.quantize8(f64(Xt))
+    Y, bound = ref.matmul4(codes, zero, inv_q, group, xc, xz, xq)
+    ref.close(ql.matmul4(q, Xt.to(DEV)), Y, bound, dtype, "rows")
+    ref.close(ql.matmul4(q, Xt.to(DEV), out_dtype=torch.float32), Y, bound, torch.float32, "rows, fp32")
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("m", [1, 9, 40])
+@pytest.mark.parametrize("x", ["narrow", "positive", "negative", "zeros", "spike", "constant"])
+def test_matmul4_zero_points_at_the_edges(ql, group, m, x):
+    """Weights of one sign (zero points 0 and -15) and rows whose range lies off 0."""
+    z = gen(m + group)
+    W = 0.05 * z(70, 300).abs()
+    W[::2] *= -1
+    X = {"narrow": 5 + 0.001 * z(m, 300), "positive": z(m, 300).abs(), "negative": -z(m, 300).abs(),
+         "zeros": torch.zeros(m, 300), "spike": torch.zeros(m, 300), "constant": torch.full((m, 300), -3.7)}[x]
+    if x == "spike":
+        X[:, 17] = 9.0
+    q = ql.quantize4(W.to(DEV), group)
+    codes, zero, inv_q = ref.quantize4(f64(W), group)
+    a, xc, xz, xq = qact(ql, X)
+    Y, bound = ref.matmul4(codes, zero, inv_q, group, xc, xz, xq)
+    ref.close(ql.matmul4(q, a), Y, bound, torch.float32, x)
+    ref.close(ql.matmul4(q, X.to(DEV)), Y, bound, torch.float32, x)
+
+
+def test_matmul4_slices_rows_that_are_not_finite_and_empty(ql):
+    z = gen(4)
+    W, buf = 0.05 * z(90, 200), z(12, 421)
+    q = ql.quantize4(W.to(DEV))
+    codes, zero, inv_q = ref.quantize4(f64(W), 64)
+    X = buf[:, 3:203].contiguous()
+    xc, xz, xq = ref.quantize8(f64(X))
+    Y, bound = ref.matmul4(codes, zero, inv_q, 64, xc, xz, xq)
+    ref.close(ql.matmul4(q, buf.to(DEV)[:, 3:203]), Y, bound, torch.float32, "slice")
+    # codes that another program padded more
+    a = ql.quantize_activations(X.to(DEV))
+    wide = torch.full((12, 448), 77, dtype=torch.int8, device=DEV)
+    wide[:, :256] = a.codes
+    ref.close(ql.matmul4(q, ql.QAct(wide, 200, a.zero, a.inv_q, a.sums)), Y, bound, torch.float32, "ld")
+    X[2, 5], X[7, 0] = float("nan"), float("inf")
+    for r in (ql.matmul4(q, X.to(DEV)).cpu(), ql.matmul4(q, X.half().to(DEV)).cpu()):
+        bad = torch.zeros(12, dtype=torch.bool)
+        bad[[2, 7]] = True
+        assert torch.isnan(r[bad]).all() and torch.isfinite(r[~bad]).all()
+    assert ql.matmul4(q, torch.empty(0, 200, device=DEV)).shape == (0, 90)
+
+
+def test_matmul4_on_its_input(ql):
+    """Y on X, as the 8-bit product allows."""
+    z = gen(6)
+    W, X = 0.05 * z(200, 200), z(20, 200)
+    q = ql.quantize4(W.to(DEV))
+    g = X.to(DEV)
+    want = ql.matmul4(q, g)
+    got = ql.matmul4(q, g, out=g)
+    assert got.data_ptr() == g.data_ptr() and torch.equal(got, want)
+
+
+# ----------------------------------------------------- convolution and scan
+CONV = [(0, 3, 70, 4), (1, 1, 1, 4), (1, 5, 300, 4), (2, 2, 33, 4), (3, 1, 64, 4), (15, 2, 130, 3),
+        (16, 3, 64, 2), (17, 1, 1000, 4), (33, 4, 257, 1), (100, 2, 96, 8), (257, 1, 50, 5), (40, 2, 64, 6),
+        (70, 3, 31, 7), (1030, 2, 36, 4)]
+
+
+def lengths_for(kind, T, B, seed):
+    if kind == "none":
+        return None
+    n = torch.randint(0, T + 1, (B,), generator=torch.Generator().manual_seed(seed), dtype=torch.int32)
+    n[0] = [0, T, T + 5][seed % 3]
+    if B > 1:
+        n[1] = [1, -4, T][seed % 3]
+    return n
+
+
+def to(t):
+    return None if t is None else t.to(DEV)
+
+
+@pytest.mark.parametrize("T,B,D,W", CONV)
+@pytest.mark.parametrize("dtype", TYPES, ids=ident)
+@pytest.mark.parametrize("lengths", ["none", "ragged"])
+def test_causal_conv(ql, T, B, D, W, dtype, lengths):
+    z = gen(T + B + D + W)
+    x, w, b, st = z(T, B, D).to(dtype), 0.5 * z(W, D), 0.2 * z(D), z(B, W - 1, D)
+    n = lengths_for(lengths, T, B, T + D)
+    silu = D % 2 == 0
+    y0 = z(T, B, D).to(dtype)
+    out, so = y0.to(DEV), torch.full((B, W - 1, D), 7.0, device=DEV)
+    ql.causal_conv(to(x), to(w), to(b), silu=silu, lengths=to(n), state_in=to(st), state_out=so, out=out)
+    y, bound, state = ref.conv(f64(x), f64(w), f64(b), silu, None if n is None else n.numpy(), f64(st))
+    on = (np.arange(T)[:, None] < ref.clamp_lengths(None if n is None else n.numpy(), T, B))[..., None]
+    ref.close(out, np.where(on, y, f64(y0)), bound, dtype, "y")
+    assert torch.equal(out.cpu()[~torch.from_numpy(on[..., 0])], y0[~torch.from_numpy(on[..., 0])])
+    assert np.array_equal(f64(so), state)
+    # the state in place
+    s = to(st)
+    ql.causal_conv(to(x), to(w), to(b), silu=silu, lengths=to(n), state_in=s, state_out=s)
+    assert torch.equal(s, so)
+    # no bias, no state
+    y, bound, _ = ref.conv(f64(x), f64(w), np.zeros(D), silu, None, np.zeros((B, W - 1, D)))
+    ref.close(ql.causal_conv(to(x), to(w), silu=silu), y, bound, dtype, "plain")
+
+
+SCAN = [(0, 2, 40, 5), (1, 1, 1, 1), (1, 7, 130, 16), (2, 2, 64, 8), (5, 1, 65, 3), (16, 3, 33, 16),
+        (31, 2, 200, 4), (33, 1, 64, 17), (100, 2, 96, 16), (257, 1, 70, 32), (130, 1, 40, 64), (90, 2, 30, 33),
+        (1030, 2, 36, 16), (700, 1, 130, 9)]
+
+
+def scan_case(T, B, D, N, dtype):
+    z = gen(T * 3 + B + D + N)
+    u = torch.Generator().manual_seed(T + N)
+    step = torch.exp(-6.9 + 4.6 * torch.rand(D, generator=u))
+    return dict(u=z(T, B, D).to(dtype), delta=(0.5 * z(T, B, D)).to(dtype),
+                A=-torch.exp(2.8 * torch.rand(N, D, generator=u)), Bm=z(T, B, N).to(dtype),
+                Cm=z(T, B, N).to(dtype), D=z(D), z=z(T, B, D).to(dtype),
+                delta_bias=torch.log(torch.expm1(step)), state=z(B, N, D))
+
+
+def scan_ref(c, lengths, softplus=True, state=True, plain=False):
+    C = c["u"].shape[2]
+    return ref.scan(f64(c["u"]), f64(c["delta"]), f64(c["A"]), f64(c["Bm"]), f64(c["Cm"]),
+                    np.zeros(C) if plain else f64(c["D"]), None if plain else f64(c["z"]),
+                    np.zeros(C) if plain else f64(c["delta_bias"]), softplus,
+                    None if lengths is None else lengths.numpy(),
+                    f64(c["state"]) if state else np.zeros(c["state"].shape))
+
+
+@pytest.mark.parametrize("T,B,D,N", SCAN)
+@pytest.mark.parametrize("dtype", TYPES, ids=ident)
+@pytest.mark.parametrize("lengths", ["none", "ragged"])
+def test_selective_scan(ql, T, B, D, N, dtype, lengths):
+    c = scan_case(T, B, D, N, dtype)
+    n = lengths_for(lengths, T, B, T + D)
+    g = {k: to(v) for k, v in c.items()}
+    y0 = torch.full((T, B, D), 3.0, dtype=dtype)
+    out, so = y0.to(DEV), torch.full((B, N, D), 7.0, device=DEV)
+    call = lambda **k: ql.selective_scan(g["u"], g["delta"], g["A"], g["Bm"], g["Cm"], D=g["D"], z=g["z"],
+                                         delta_bias=g["delta_bias"], lengths=to(n), **k)
+    call(state_in=g["state"], state_out=so, out=out)
+    y, by, h, bh = scan_ref(c, n)
+    on = torch.from_numpy(np.arange(T)[:, None] < ref.clamp_lengths(None if n is None else n.numpy(), T, B))
+    assert (out.cpu()[~on] == 3).all()
+    ref.close(out.cpu()[on], y[on.numpy()], by[on.numpy()], dtype, "y")
+    ref.close(so, h, bh, torch.float32, "state")
+    s = g["state"].clone()  # in place: the same bits
+    y2 = call(state_in=s, state_out=s, out=y0.to(DEV))
+    assert torch.equal(s, so) and torch.equal(y2, out)
+    # nothing but the recurrence, and no softplus: steps of exp(delta - 3)
+    c["delta"] = torch.exp(c["delta"].float() - 3).to(dtype)
+    y, by, h, bh = scan_ref(c, None, softplus=False, state=False, plain=True)
+    out = ql.selective_scan(g["u"], to(c["delta"]), g["A"], g["Bm"], g["Cm"], softplus=False)
+    ref.close(out, y, by, dtype, "plain y")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=ident)
+@pytest.mark.parametrize("T,B,D,N", [(37, 3, 70, 5), (300, 2, 64, 16), (1, 4, 96, 16)])
+def test_ssm_layouts_and_results_on_inputs(ql, dtype, T, B, D, N):
+    """Batch-major tensors and column slices of wider buffers off any alignment, y on
+    u, delta or z: the bits of dense time-major tensors."""
+    c = scan_case(T, B, D, N, dtype)
+    g = {k: to(v) for k, v in c.items()}
+    dense = ql.selective_scan(g["u"], g["delta"], g["A"], g["Bm"], g["Cm"], D=g["D"], z=g["z"],
+                              delta_bias=g["delta_bias"], state_in=g["state"])
+    xz = torch.zeros(B, T, 2 * D + 3, dtype=dtype, device=DEV)   # [batch][time]: x and z
+    dbc = torch.zeros(T, B, D + 2 * N + 1, dtype=dtype, device=DEV)  # [time][batch]: delta, B, C
+    xz[:, :, 1:1 + D] = g["u"].transpose(0, 1)
+    xz[:, :, 1 + D:1 + 2 * D] = g["z"].transpose(0, 1)
+    dbc[:, :, :D], dbc[:, :, D:D + N], dbc[:, :, D + N:D + 2 * N] = g["delta"], g["Bm"], g["Cm"]
+    for k in ("u", "delta", "z", None):
+        a, b = xz.clone(), dbc.clone()
+        v = dict(u=a[:, :, 1:1 + D].transpose(0, 1), z=a[:, :, 1 + D:1 + 2 * D].transpose(0, 1),
+                 delta=b[:, :, :D], Bm=b[:, :, D:D + N], Cm=b[:, :, D + N:D + 2 * N])
+        y = ql.selective_scan(v["u"], v["delta"], g["A"], v["Bm"], v["Cm"], D=g["D"], z=v["z"],
+                              delta_bias=g["delta_bias"], state_in=g["state"],
+                              out=v[k] if k else None)
+        assert torch.equal(y, dense)
+        assert not a[:, :, 0].any() and not a[:, :, 1 + 2 * D:].any() and not b[:, :, D + 2 * N:].any()
+    w = to(gen(3)(4, D))
+    a = xz.clone()
+    y = ql.causal_conv(a[:, :, 1:1 + D].transpose(0, 1), w, out=a[:, :, 1 + D:1 + 2 * D].transpose(0, 1))
+    assert torch.equal(y, ql.causal_conv(g["u"], w))
+    assert torch.equal(a[:, :, 1:1 + D], xz[:, :, 1:1 + D])
+
+
+@pytest.mark.parametrize("cut", [1, 16, 100])
+def test_ssm_chunks_of_a_stream(ql, cut):
+    """A sequence fed in pieces through its state: the convolution bit for bit, the scan
+    to the roundings of both ways."""
+    T, B, D, N = 230, 2, 70, 16
+    c = scan_case(T, B, D, N, torch.float32)
+    g = {k: to(v) for k, v in c.items()}
+    w = to(0.5 * gen(1)(4, D))
+    whole = ql.causal_conv(g["u"], w)
+    y, by, h, bh = scan_ref(c, None, state=False)
+    cs, hs = torch.zeros(B, 3, D, device=DEV), torch.zeros(B, N, D, device=DEV)
+    outs, ys = [], []
+    for t in range(0, T, cut):
+        p = slice(t, t + cut)
+        outs.append(ql.causal_conv(g["u"][p], w, state_in=cs, state_out=cs))
+        ys.append(ql.selective_scan(g["u"][p], g["delta"][p], g["A"], g["Bm"][p], g["Cm"][p], D=g["D"],
+                                    z=g["z"][p], delta_bias=g["delta_bias"], state_in=hs, state_out=hs))
+    assert torch.equal(torch.cat(outs), whole)
+    ref.close(torch.cat(ys), y, by, torch.float32, "y")
+    ref.close(hs, h, bh, torch.float32, "state")
+
+
+def test_scan_extremes(ql):
+    """Steps of 0, steps that end a state at once, and values that are not finite, which
+    stay in their channel and sequence."""
+    T, B, D, N = 150, 2, 70, 8
+    c = scan_case(T, B, D, N, torch.float32)
+    c["delta"][:40] = -60.0     # softplus ~ 0: the state stays
+    c["delta"][60] = 80.0       # exp(-80 A): the state is gone
+    g = {k: to(v) for k, v in c.items()}
+    run = lambda: ql.selective_scan(g["u"], g["delta"], g["A"], g["Bm"], g["Cm"], D=g["D"], z=g["z"],
+                                    delta_bias=g["delta_bias"], state_in=g["state"])
+    y, by, _, _ = scan_ref(c, None)
+    ref.close(run(), y, by, torch.float32, "y")
+    g["u"][100, 1, 7] = float("nan")
+    g["delta"][20, 0, 3] = float("inf")
+    a = run().cpu()
+    on = torch.ones(T, B, D, dtype=torch.bool)
+    on[100:, 1, 7] = False
+    on[20:, 0, 3] = False
+    assert torch.isnan(a[100:, 1, 7]).all()
+    ref.close(a[on], y[on.numpy()], by[on.numpy()], torch.float32, "others")
