@@ -38,15 +38,35 @@ __device__ __forceinline__ void store_n(T *p, const float (&v)[N]) {
   }
 }
 
+// Sums over the wave, in every lane: DPP shifts within rows of 16 lanes, then row
+// broadcasts, the result read from lane 63.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_f32(float v) {
+  return __int_as_float(dpp_i<CTRL, ROWS>(0, __float_as_int(v)));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_f64(double v) {
+  return __hiloint2double(dpp_i<CTRL, ROWS>(0, __double2hiint(v)),
+                          dpp_i<CTRL, ROWS>(0, __double2loint(v)));
+}
 __device__ __forceinline__ double wave_sum_f64(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  v += dpp_f64<kRowShr1, 0xf>(v);
+  v += dpp_f64<kRowShr2, 0xf>(v);
+  v += dpp_f64<kRowShr4, 0xf>(v);
+  v += dpp_f64<kRowShr8, 0xf>(v);
+  v += dpp_f64<kRowBcast15, 0xa>(v);
+  v += dpp_f64<kRowBcast31, 0xc>(v);
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), 63),
+                          __builtin_amdgcn_readlane(__double2loint(v), 63));
 }
 __device__ __forceinline__ float wave_sum_f32(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  v += dpp_f32<kRowShr1, 0xf>(v);
+  v += dpp_f32<kRowShr2, 0xf>(v);
+  v += dpp_f32<kRowShr4, 0xf>(v);
+  v += dpp_f32<kRowShr8, 0xf>(v);
+  v += dpp_f32<kRowBcast15, 0xa>(v);
+  v += dpp_f32<kRowBcast31, 0xc>(v);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 }  // namespace ql

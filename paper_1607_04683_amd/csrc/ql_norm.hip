@@ -12,6 +12,7 @@
 #include "ql_launch.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ql {
 
@@ -33,7 +34,174 @@ __device__ __forceinline__ F block_sum(F v, F *s) {
   return v;
 }
 
+// A row held by WAVES waves, PER values a thread in vectors of VEC: vector k of
+// thread t is values (k 64 WAVES + t) VEC .. + VEC - 1.
+template <int VEC, int PER, int WAVES>
+struct RowSlots {
+  static constexpr int kVecs = PER / VEC;
+  static constexpr int kThreads = 64 * WAVES;
+  static constexpr int kCols = PER * kThreads;  // the longest row
+  static __device__ __forceinline__ int col(int k, int t) { return (k * kThreads + t) * VEC; }
+};
+
 }  // namespace
+
+// The row in registers: read once.  One wave per row up to 1024 values, four
+// up to 4096, 16 up to 16384 (workgroups of four waves, or 16).
+template <class T, int VEC, int PER, int WAVES>
+__global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_rms_norm_reg(NormArgs a) {
+  typedef RowSlots<VEC, PER, WAVES> S;
+  constexpr int kBlock = WAVES == 16 ? 1024 : 256, kRows = kBlock / S::kThreads;
+  __shared__ double ssum[16];
+  __shared__ float slo[16], shi[16];
+  __shared__ int sbad[16], scodes[16];
+  const int t = threadIdx.x % S::kThreads, wave = threadIdx.x >> 6;
+  const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / S::kThreads;
+  if (WAVES == 1 && row >= a.rows) return;  // (no barriers in this form)
+  const int n = (int)a.cols;
+  const T *x = static_cast<const T *>(a.x) + row * a.ldx;
+  const T *r = static_cast<const T *>(a.residual) + row * a.ldr;
+
+  float v[PER];
+#pragma unroll
+  for (int k = 0; k < S::kVecs; ++k) {
+    const int c = S::col(k, t);
+    float xv[VEC];
+    if (c < n) {
+      load_n<VEC>(xv, x + c);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) xv[i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[k * VEC + i] = xv[i];
+  }
+  if (a.residual) {
+    float rv[PER];
+#pragma unroll
+    for (int k = 0; k < S::kVecs; ++k) {
+      const int c = S::col(k, t);
+      float q[VEC];
+      if (c < n) {
+        load_n<VEC>(q, r + c);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) q[i] = 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) rv[k * VEC + i] = q[i];
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) v[i] = (float)(T)(v[i] + rv[i]);
+  }
+  double ss = 0.0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) ss = __builtin_fma((double)v[i], (double)v[i], ss);
+  ss = wave_sum_f64(ss);
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) ssum[wave] = ss;
+    __syncthreads();
+    ss = ssum[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) ss += ssum[w];
+  }
+  const float rstd = (float)(1.0 / sqrt(ss / (double)n + a.eps));
+  if (a.rstd && t == 0) a.rstd[row] = rstd;
+  if (a.sum) {
+    T *o = static_cast<T *>(a.sum) + row * a.lds;
+#pragma unroll
+    for (int k = 0; k < S::kVecs; ++k) {
+      const int c = S::col(k, t);
+      float q[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) q[i] = v[k * VEC + i];
+      if (c < n) store_n<VEC>(o + c, q);
+    }
+  }
+  if (!a.y && !a.codes) return;
+#pragma unroll
+  for (int k = 0; k < S::kVecs; ++k) {
+    const int c = S::col(k, t);
+    float w[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) w[i] = 1.0f;
+    if (a.weight && c < n) load_n<VEC>(w, a.weight + c);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[k * VEC + i] = v[k * VEC + i] * rstd * w[i];
+  }
+  if (a.y) {
+    T *o = static_cast<T *>(a.y) + row * a.ldy;
+#pragma unroll
+    for (int k = 0; k < S::kVecs; ++k) {
+      const int c = S::col(k, t);
+      float q[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) q[i] = v[k * VEC + i];
+      if (c < n) store_n<VEC>(o + c, q);
+    }
+  }
+  if (!a.codes) return;
+  float lo = INFINITY, hi = -INFINITY, nan = 0.0f;
+#pragma unroll
+  for (int k = 0; k < S::kVecs; ++k)
+    if (S::col(k, t) < n) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        lo = fminf(lo, v[k * VEC + i]);
+        hi = fmaxf(hi, v[k * VEC + i]);
+        nan = __builtin_fmaf(v[k * VEC + i], 0.0f, nan);  // NaN where one is not finite
+      }
+    }
+  lo = wave_min(lo);
+  hi = wave_max(hi);
+  bool bad = __any(nan != nan);
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) slo[wave] = lo, shi[wave] = hi, sbad[wave] = bad;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      lo = fminf(lo, slo[w]);
+      hi = fmaxf(hi, shi[w]);
+      bad |= sbad[w] != 0;
+    }
+  }
+  const QParams p = bad ? QParams{0.0, 0, __builtin_nanf(""), 0.0} : make_qparams(lo, hi);
+  int8_t *o = a.codes + row * a.ldc;
+  int sum = 0;
+#pragma unroll
+  for (int k = 0; k < S::kVecs; ++k) {
+    const int c = S::col(k, t);
+    if (c < n) {
+      uint32_t word[(VEC + 3) / 4] = {};
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        const int code = bad ? 0 : encode(v[k * VEC + i], p.q, p.z);
+        sum += code;
+        word[i / 4] |= (uint32_t)(code ^ 0x80) << (8 * (i % 4));
+      }
+      if constexpr (VEC == 1)
+        o[c] = (int8_t)word[0];
+      else if constexpr (VEC == 4)
+        *reinterpret_cast<uint32_t *>(o + c) = word[0];
+      else
+        *reinterpret_cast<uint2 *>(o + c) = make_uint2(word[0], word[1]);
+    }
+  }
+  for (int64_t c = n + t; c < a.ldc; c += S::kThreads) o[c] = 0;
+  sum = wave_sum(sum);
+  if constexpr (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) scodes[wave] = sum;
+    __syncthreads();
+    sum = scodes[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) sum += scodes[w];
+  }
+  if (t == 0) {
+    a.zero[row] = p.z;
+    a.inv_q[row] = p.inv_q;
+    a.sums[row] = sum;
+  }
+}
 
 // One workgroup per row, the row read three times (sum of squares, range, result);
 // an element is read and then written by one thread, so results may lie on
@@ -115,6 +283,123 @@ __global__ __launch_bounds__(256) void k_rms_norm(NormArgs a) {
   }
 }
 
+// Both gradients with the rows in registers: every group of WAVES waves takes rows
+// `groups` apart, its share of dweight in registers, which the workgroup adds up
+// and leaves in its row of `part`.  The next row's values are loaded while this
+// one's sum is on its way, where the registers hold both.
+template <class T, int VEC, int PER, int WAVES>
+__global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_rms_norm_grad(
+    NormGradArgs a, float *__restrict__ part) {
+  typedef RowSlots<VEC, PER, WAVES> S;
+  constexpr int kBlock = WAVES == 16 ? 1024 : 256, kRows = kBlock / S::kThreads;
+  constexpr bool kAhead = PER * WAVES < 256;
+  __shared__ float ssum[2][16];
+  __shared__ float sdw[WAVES == 1 ? 3 * S::kCols : 1];
+  const int t = threadIdx.x % S::kThreads, wave = threadIdx.x >> 6;
+  const int n = (int)a.cols;
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  const float rn = 1.0f / (float)n;
+  float w[PER], dw[PER], dy[PER], v[PER], ds[PER];
+  float rstd = 0.0f;
+  // a row's values; nothing past the row's end or the last row
+  auto get = [&](float(&o)[PER], const void *base, int64_t ld, int64_t row) {
+    const T *p = static_cast<const T *>(base) + row * ld;
+#pragma unroll
+    for (int k = 0; k < S::kVecs; ++k) {
+      const int c = S::col(k, t);
+      float q[VEC];
+      if (c < n) {
+        load_n<VEC>(q, p + c);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) q[i] = 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) o[k * VEC + i] = q[i];
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < S::kVecs; ++k) {
+    const int c = S::col(k, t);
+    float q[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) q[i] = 1.0f;
+    if (a.weight && c < n) load_n<VEC>(q, a.weight + c);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) w[k * VEC + i] = q[i], dw[k * VEC + i] = 0.0f;
+  }
+  int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / S::kThreads;
+  if (row < a.rows) {
+    get(dy, a.dy, a.lddy, row);
+    get(v, a.v, a.ldv, row);
+    rstd = a.rstd[row];
+  }
+  for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
+    if (a.dsum) get(ds, a.dsum, a.ldds, row);
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      dw[i] = __builtin_fmaf(dy[i], v[i] * rstd, dw[i]);
+      dy[i] *= w[i];
+      s = __builtin_fmaf(dy[i], v[i], s);
+    }
+    float dx[PER];
+    const float c0 = rstd * rstd * rstd * rn, r0 = rstd;
+    float g[PER], vv[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) g[i] = dy[i] * r0, vv[i] = v[i] * c0;
+    const int64_t next = row + step;
+    auto load_next = [&] {
+      if (next < a.rows) {
+        get(dy, a.dy, a.lddy, next);
+        get(v, a.v, a.ldv, next);
+        rstd = a.rstd[next];
+      }
+    };
+    if constexpr (kAhead) load_next();
+    s = wave_sum_f32(s);
+    if constexpr (WAVES > 1) {  // two places in turn: one barrier a row
+      if ((threadIdx.x & 63) == 0) ssum[turn][wave] = s;
+      __syncthreads();
+      s = ssum[turn][0];
+#pragma unroll
+      for (int q = 1; q < WAVES; ++q) s += ssum[turn][q];
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      dx[i] = __builtin_fmaf(-vv[i], s, g[i]);
+      if (a.dsum) dx[i] += ds[i];
+    }
+    T *o = static_cast<T *>(a.dx) + row * a.lddx;
+#pragma unroll
+    for (int k = 0; k < S::kVecs; ++k) {
+      const int c = S::col(k, t);
+      float q[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) q[i] = dx[k * VEC + i];
+      if (c < n) store_n<VEC>(o + c, q);
+    }
+    if constexpr (!kAhead) load_next();
+  }
+  if (!a.dweight) return;
+  if constexpr (WAVES == 1) {
+    if (wave > 0)
+#pragma unroll
+      for (int i = 0; i < PER; ++i) sdw[(wave - 1) * S::kCols + i * 64 + t] = dw[i];
+    __syncthreads();
+    if (wave > 0) return;
+    for (int q = 0; q < 3; ++q)
+#pragma unroll
+      for (int i = 0; i < PER; ++i) dw[i] += sdw[q * S::kCols + i * 64 + t];
+  }
+  float *o = part + (int64_t)blockIdx.x * n;
+#pragma unroll
+  for (int k = 0; k < S::kVecs; ++k)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i)
+      if (S::col(k, t) < n) o[S::col(k, t) + i] = dw[k * VEC + i];
+}
+
 // dx of one row per workgroup:
 //   dx = rstd g - v rstd^3 / n sum(g v) + dsum,  g = w dy
 template <class T>
@@ -155,50 +440,128 @@ __global__ __launch_bounds__(256) void k_rms_norm_dw(NormGradArgs a, float *__re
     s = __builtin_fmaf((float)dy[r * a.lddy + i], (float)v[r * a.ldv + i] * a.rstd[r], s);
   part[(int64_t)blockIdx.y * a.cols + i] = s;
 }
-__global__ __launch_bounds__(256) void k_rms_norm_dw_join(const float *__restrict__ part, int parts,
-                                                          int64_t cols, float *__restrict__ dw) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= cols) return;
-  float s = 0.0f;
-  for (int p = 0; p < parts; ++p) s += part[(int64_t)p * cols + i];
-  dw[i] = s;
+// dweight = the sum of the partial ones, 64 columns a workgroup: wave w adds up
+// rows w, w + 16, ..., then the 16 sums are added in order.
+__global__ __launch_bounds__(1024) void k_rms_norm_dw_join(const float *__restrict__ part,
+                                                           int parts, int64_t cols,
+                                                           float *__restrict__ dw) {
+  __shared__ float s[16][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t i = (int64_t)blockIdx.x * 64 + lane;
+  float v = 0.0f;
+  if (i < cols) {
+#pragma unroll 8
+    for (int p = w; p < parts; p += 16) v += part[(int64_t)p * cols + i];
+  }
+  s[w][lane] = v;
+  __syncthreads();
+  if (w == 0 && i < cols) {
+    for (int q = 1; q < 16; ++q) v += s[q][lane];
+    dw[i] = v;
+  }
 }
 
 // ---------------------------------------------------------------- launchers
 static inline unsigned blocks_for(int64_t n, int per) { return (unsigned)((n + per - 1) / per); }
 
+// Whether rows of a matrix (null: none) start on multiples of `bytes`.
+static bool rows_aligned(const void *p, int64_t ld, size_t e, size_t bytes) {
+  return !p || (reinterpret_cast<uintptr_t>(p) % bytes == 0 && (size_t)ld * e % bytes == 0);
+}
+
+// The form of a row in registers by its length and alignment: calls f with T, VEC,
+// PER and WAVES as types; false where none holds it.
+template <int N>
+using Int = std::integral_constant<int, N>;
+template <class T, class F>
+static bool by_row(int64_t cols, bool aligned, F f) {
+  constexpr int V = 16 / sizeof(T);
+  auto waves = [&](auto vec, auto w) {
+    constexpr int VEC = decltype(vec)::value, W = decltype(w)::value;
+    if (cols <= 8 * 64 * W)
+      f(vec, Int<8>(), w);
+    else
+      f(vec, Int<16>(), w);
+  };
+  auto row = [&](auto vec) {
+    if (cols <= 1024)
+      waves(vec, Int<1>());
+    else if (cols <= 4096)
+      waves(vec, Int<4>());
+    else
+      waves(vec, Int<16>());
+  };
+  if (cols > 16384) return false;
+  if (aligned && cols % V == 0)
+    row(Int<V>());
+  else
+    row(Int<1>());
+  return true;
+}
+constexpr int block_of(int waves) { return waves == 16 ? 1024 : 256; }
+
+template <class T>
+static void run_rms_norm(const NormArgs &a, hipStream_t s) {
+  constexpr size_t e = sizeof(T);
+  const bool aligned = rows_aligned(a.x, a.ldx, e, 16) && rows_aligned(a.residual, a.ldr, e, 16) &&
+                       rows_aligned(a.sum, a.lds, e, 16) && rows_aligned(a.y, a.ldy, e, 16) &&
+                       rows_aligned(a.codes, a.ldc, 1, 8) && rows_aligned(a.weight, 0, 4, 16);
+  const bool done = by_row<T>(a.cols, aligned, [&](auto vec, auto per, auto w) {
+    constexpr int W = decltype(w)::value;
+    hipLaunchKernelGGL((k_rms_norm_reg<T, decltype(vec)::value, decltype(per)::value, W>),
+                       dim3(blocks_for(a.rows, block_of(W) / (64 * W))), dim3(block_of(W)), 0, s, a);
+  });
+  if (!done) hipLaunchKernelGGL(k_rms_norm<T>, dim3((unsigned)a.rows), dim3(256), 0, s, a);
+}
 hipError_t launch_rms_norm(int type, const NormArgs &a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
-  auto kern = type == 0 ? k_rms_norm<float> : type == 1 ? k_rms_norm<f16> : k_rms_norm<bf16>;
-  hipLaunchKernelGGL(kern, dim3((unsigned)a.rows), dim3(256), 0, s, a);
+  if (type == 0)
+    run_rms_norm<float>(a, s);
+  else if (type == 1)
+    run_rms_norm<f16>(a, s);
+  else
+    run_rms_norm<bf16>(a, s);
   return hipGetLastError();
 }
 
-// Bands of rows of the partial dweight.
+// Workgroups of the backward pass, each with a row of the partial dweight.
 static int grad_parts(int64_t rows) {
-  return (int)std::min<int64_t>(256, std::max<int64_t>(1, rows / 16));
+  return (int)std::min<int64_t>(512, std::max<int64_t>(1, rows / 4));
 }
 size_t rms_norm_backward_ws(int64_t rows, int64_t cols) {
   return align_up((size_t)grad_parts(rows) * (size_t)cols * sizeof(float), 256);
 }
 
-hipError_t launch_rms_norm_backward(int type, const NormGradArgs &a, float *part, hipStream_t s) {
-  if (a.dweight) {
-    const int parts = grad_parts(a.rows);
-    const int64_t per = (a.rows + parts - 1) / parts;
-    auto kern = type == 0 ? k_rms_norm_dw<float>
-                : type == 1 ? k_rms_norm_dw<f16>
-                            : k_rms_norm_dw<bf16>;
-    hipLaunchKernelGGL(kern, dim3(blocks_for(a.cols, 256), parts), dim3(256), 0, s, a, part, per);
-    hipLaunchKernelGGL(k_rms_norm_dw_join, dim3(blocks_for(a.cols, 256)), dim3(256), 0, s, part,
+template <class T>
+static void run_rms_norm_backward(const NormGradArgs &a, float *part, hipStream_t s) {
+  constexpr size_t e = sizeof(T);
+  const int parts = grad_parts(a.rows);
+  const bool aligned = rows_aligned(a.dy, a.lddy, e, 16) && rows_aligned(a.v, a.ldv, e, 16) &&
+                       rows_aligned(a.dsum, a.ldds, e, 16) && rows_aligned(a.dx, a.lddx, e, 16) &&
+                       rows_aligned(a.weight, 0, 4, 16);
+  const bool done = by_row<T>(a.cols, aligned, [&](auto vec, auto per, auto w) {
+    constexpr int W = decltype(w)::value;
+    hipLaunchKernelGGL((k_rms_norm_grad<T, decltype(vec)::value, decltype(per)::value, W>), dim3(parts),
+                       dim3(block_of(W)), 0, s, a, part);
+  });
+  if (!done) {  // dweight first: dx may lie on an input
+    if (a.dweight)
+      hipLaunchKernelGGL(k_rms_norm_dw<T>, dim3(blocks_for(a.cols, 256), parts), dim3(256), 0, s, a,
+                         part, (a.rows + parts - 1) / parts);
+    if (a.rows > 0)
+      hipLaunchKernelGGL(k_rms_norm_dx<T>, dim3((unsigned)a.rows), dim3(256), 0, s, a);
+  }
+  if (a.dweight)
+    hipLaunchKernelGGL(k_rms_norm_dw_join, dim3(blocks_for(a.cols, 64)), dim3(1024), 0, s, part,
                        parts, a.cols, a.dweight);
-  }
-  if (a.rows > 0) {
-    auto kern = type == 0 ? k_rms_norm_dx<float>
-                : type == 1 ? k_rms_norm_dx<f16>
-                            : k_rms_norm_dx<bf16>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)a.rows), dim3(256), 0, s, a);
-  }
+}
+hipError_t launch_rms_norm_backward(int type, const NormGradArgs &a, float *part, hipStream_t s) {
+  if (type == 0)
+    run_rms_norm_backward<float>(a, part, s);
+  else if (type == 1)
+    run_rms_norm_backward<f16>(a, part, s);
+  else
+    run_rms_norm_backward<bf16>(a, part, s);
   return hipGetLastError();
 }
 
