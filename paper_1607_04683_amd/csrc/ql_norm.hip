@@ -42,16 +42,60 @@ struct RowSlots {
   static constexpr int kThreads = 64 * WAVES;
   static constexpr int kCols = PER * kThreads;  // the longest row
   static __device__ __forceinline__ int col(int k, int t) { return (k * kThreads + t) * VEC; }
+  // The thread's values of a row of n, 0 past its end.  TAIL: n is no multiple of
+  // VEC; the one vector that the end cuts comes value by value, after the others
+  // are in flight.
+  template <bool TAIL, class T>
+  static __device__ __forceinline__ void load(float (&v)[PER], const T *p, int n, int t) {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      const int c = col(k, t);
+      float q[VEC];
+      if (TAIL ? c + VEC <= n : c < n) {
+        load_n<VEC>(q, p + c);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) q[i] = 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[k * VEC + i] = q[i];
+    }
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        const int c = col(k, t);
+        if (c < n && c + VEC > n)
+#pragma unroll
+          for (int i = 0; i < VEC - 1; ++i)
+            if (c + i < n) v[k * VEC + i] = (float)p[c + i];
+      }
+    }
+  }
+  template <bool TAIL, class T>
+  static __device__ __forceinline__ void store(T *p, const float (&v)[PER], int n, int t) {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      const int c = col(k, t);
+      float q[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) q[i] = v[k * VEC + i];
+      if (TAIL ? c + VEC <= n : c < n) store_n<VEC>(p + c, q);
+      if (TAIL && c < n && c + VEC > n)
+#pragma unroll
+        for (int i = 0; i < VEC - 1; ++i)
+          if (c + i < n) p[c + i] = (T)q[i];
+    }
+  }
 };
 
 }  // namespace
 
 // The row in registers: read once.  One wave per row up to 1024 values, four
-// up to 4096, 16 up to 16384 (workgroups of four waves, or 16).
-template <class T, int VEC, int PER, int WAVES>
-__global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_rms_norm_reg(NormArgs a) {
+// up to 2048, eight up to 4096, 16 up to 16384 (workgroups of four waves at least).
+template <class T, int VEC, int PER, int WAVES, bool TAIL>
+__global__ __launch_bounds__((WAVES == 1 ? 256 : 64 * WAVES)) void k_rms_norm_reg(NormArgs a) {
   typedef RowSlots<VEC, PER, WAVES> S;
-  constexpr int kBlock = WAVES == 16 ? 1024 : 256, kRows = kBlock / S::kThreads;
+  constexpr int kBlock = (WAVES == 1 ? 256 : 64 * WAVES), kRows = kBlock / S::kThreads;
   __shared__ double ssum[16];
   __shared__ float slo[16], shi[16];
   __shared__ int sbad[16], scodes[16];
@@ -63,34 +107,10 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_rms_norm_reg(NormA
   const T *r = static_cast<const T *>(a.residual) + row * a.ldr;
 
   float v[PER];
-#pragma unroll
-  for (int k = 0; k < S::kVecs; ++k) {
-    const int c = S::col(k, t);
-    float xv[VEC];
-    if (c < n) {
-      load_n<VEC>(xv, x + c);
-    } else {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) xv[i] = 0.0f;
-    }
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) v[k * VEC + i] = xv[i];
-  }
+  S::template load<TAIL>(v, x, n, t);
   if (a.residual) {
     float rv[PER];
-#pragma unroll
-    for (int k = 0; k < S::kVecs; ++k) {
-      const int c = S::col(k, t);
-      float q[VEC];
-      if (c < n) {
-        load_n<VEC>(q, r + c);
-      } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) q[i] = 0.0f;
-      }
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) rv[k * VEC + i] = q[i];
-    }
+    S::template load<TAIL>(rv, r, n, t);
 #pragma unroll
     for (int i = 0; i < PER; ++i) v[i] = (float)(T)(v[i] + rv[i]);
   }
@@ -107,50 +127,26 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_rms_norm_reg(NormA
   }
   const float rstd = (float)(1.0 / sqrt(ss / (double)n + a.eps));
   if (a.rstd && t == 0) a.rstd[row] = rstd;
-  if (a.sum) {
-    T *o = static_cast<T *>(a.sum) + row * a.lds;
-#pragma unroll
-    for (int k = 0; k < S::kVecs; ++k) {
-      const int c = S::col(k, t);
-      float q[VEC];
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) q[i] = v[k * VEC + i];
-      if (c < n) store_n<VEC>(o + c, q);
-    }
-  }
+  if (a.sum) S::template store<TAIL>(static_cast<T *>(a.sum) + row * a.lds, v, n, t);
   if (!a.y && !a.codes) return;
+  if (a.weight) {
+    float w[PER];
+    S::template load<TAIL>(w, a.weight, n, t);
 #pragma unroll
-  for (int k = 0; k < S::kVecs; ++k) {
-    const int c = S::col(k, t);
-    float w[VEC];
+    for (int i = 0; i < PER; ++i) v[i] = v[i] * rstd * w[i];
+  } else {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) w[i] = 1.0f;
-    if (a.weight && c < n) load_n<VEC>(w, a.weight + c);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) v[k * VEC + i] = v[k * VEC + i] * rstd * w[i];
+    for (int i = 0; i < PER; ++i) v[i] = v[i] * rstd;
   }
-  if (a.y) {
-    T *o = static_cast<T *>(a.y) + row * a.ldy;
-#pragma unroll
-    for (int k = 0; k < S::kVecs; ++k) {
-      const int c = S::col(k, t);
-      float q[VEC];
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) q[i] = v[k * VEC + i];
-      if (c < n) store_n<VEC>(o + c, q);
-    }
-  }
+  if (a.y) S::template store<TAIL>(static_cast<T *>(a.y) + row * a.ldy, v, n, t);
   if (!a.codes) return;
   float lo = INFINITY, hi = -INFINITY, nan = 0.0f;
 #pragma unroll
-  for (int k = 0; k < S::kVecs; ++k)
-    if (S::col(k, t) < n) {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        lo = fminf(lo, v[k * VEC + i]);
-        hi = fmaxf(hi, v[k * VEC + i]);
-        nan = __builtin_fmaf(v[k * VEC + i], 0.0f, nan);  // NaN where one is not finite
-      }
+  for (int e = 0; e < PER; ++e)
+    if (S::col(e / VEC, t) + e % VEC < n) {
+      lo = fminf(lo, v[e]);
+      hi = fmaxf(hi, v[e]);
+      nan = __builtin_fmaf(v[e], 0.0f, nan);  // NaN where one is not finite
     }
   lo = wave_min(lo);
   hi = wave_max(hi);
@@ -165,28 +161,40 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_rms_norm_reg(NormA
       bad |= sbad[w] != 0;
     }
   }
+  // a row with a value that is not finite: every code 0 (Q = 0, z = 0)
   const QParams p = bad ? QParams{0.0, 0, __builtin_nanf(""), 0.0} : make_qparams(lo, hi);
+  const FastEncode f = bad ? FastEncode{0.0f, 0.0f, 2.0f} : fast_encode(p, lo, hi);
   int8_t *o = a.codes + row * a.ldc;
-  int sum = 0;
+  uint32_t codesum = 0;
 #pragma unroll
   for (int k = 0; k < S::kVecs; ++k) {
     const int c = S::col(k, t);
-    if (c < n) {
-      uint32_t word[(VEC + 3) / 4] = {};
+    float q[VEC];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        const int code = bad ? 0 : encode(v[k * VEC + i], p.q, p.z);
-        sum += code;
-        word[i / 4] |= (uint32_t)(code ^ 0x80) << (8 * (i % 4));
+    for (int i = 0; i < VEC; ++i) q[i] = bad ? 0.0f : v[k * VEC + i];
+    uint32_t w[VEC / 4];
+    encode_words<VEC>(q, p, f, w);
+    if (TAIL ? c + VEC <= n : c < n) {
+      typedef uint32_t vec __attribute__((ext_vector_type(VEC / 4)));
+      typedef vec any __attribute__((aligned(1)));
+      vec o4;
+#pragma unroll
+      for (int i = 0; i < VEC / 4; ++i) {
+        codesum = add_codes(w[i], codesum);
+        o4[i] = w[i] ^ 0x80808080u;
       }
-      if constexpr (VEC == 1)
-        o[c] = (int8_t)word[0];
-      else if constexpr (VEC == 4)
-        *reinterpret_cast<uint32_t *>(o + c) = word[0];
-      else
-        *reinterpret_cast<uint2 *>(o + c) = make_uint2(word[0], word[1]);
+      *reinterpret_cast<any *>(o + c) = o4;
+    } else if (TAIL) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i)
+        if (c + i < n) {
+          const uint32_t code = (w[i / 4] >> (8 * (i % 4))) & 255u;
+          codesum += code;
+          o[c + i] = (int8_t)(code ^ 0x80u);
+        }
     }
   }
+  int sum = (int)codesum;
   for (int64_t c = n + t; c < a.ldc; c += S::kThreads) o[c] = 0;
   sum = wave_sum(sum);
   if constexpr (WAVES > 1) {
@@ -287,11 +295,11 @@ __global__ __launch_bounds__(256) void k_rms_norm(NormArgs a) {
 // `groups` apart, its share of dweight in registers, which the workgroup adds up
 // and leaves in its row of `part`.  The next row's values are loaded while this
 // one's sum is on its way, where the registers hold both.
-template <class T, int VEC, int PER, int WAVES>
-__global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_rms_norm_grad(
+template <class T, int VEC, int PER, int WAVES, bool TAIL>
+__global__ __launch_bounds__((WAVES == 1 ? 256 : 64 * WAVES)) void k_rms_norm_grad(
     NormGradArgs a, float *__restrict__ part) {
   typedef RowSlots<VEC, PER, WAVES> S;
-  constexpr int kBlock = WAVES == 16 ? 1024 : 256, kRows = kBlock / S::kThreads;
+  constexpr int kBlock = (WAVES == 1 ? 256 : 64 * WAVES), kRows = kBlock / S::kThreads;
   constexpr bool kAhead = PER * WAVES < 256;
   __shared__ float ssum[2][16];
   __shared__ float sdw[WAVES == 1 ? 3 * S::kCols : 1];
@@ -301,33 +309,17 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_rms_norm_grad(
   const float rn = 1.0f / (float)n;
   float w[PER], dw[PER], dy[PER], v[PER], ds[PER];
   float rstd = 0.0f;
-  // a row's values; nothing past the row's end or the last row
   auto get = [&](float(&o)[PER], const void *base, int64_t ld, int64_t row) {
-    const T *p = static_cast<const T *>(base) + row * ld;
-#pragma unroll
-    for (int k = 0; k < S::kVecs; ++k) {
-      const int c = S::col(k, t);
-      float q[VEC];
-      if (c < n) {
-        load_n<VEC>(q, p + c);
-      } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) q[i] = 0.0f;
-      }
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) o[k * VEC + i] = q[i];
-    }
+    S::template load<TAIL>(o, static_cast<const T *>(base) + row * ld, n, t);
   };
+  if (a.weight) {
+    S::template load<TAIL>(w, a.weight, n, t);
+  } else {
 #pragma unroll
-  for (int k = 0; k < S::kVecs; ++k) {
-    const int c = S::col(k, t);
-    float q[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) q[i] = 1.0f;
-    if (a.weight && c < n) load_n<VEC>(q, a.weight + c);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) w[k * VEC + i] = q[i], dw[k * VEC + i] = 0.0f;
+    for (int i = 0; i < PER; ++i) w[i] = 1.0f;
   }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) dw[i] = 0.0f;
   int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / S::kThreads;
   if (row < a.rows) {
     get(dy, a.dy, a.lddy, row);
@@ -370,15 +362,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_rms_norm_grad(
       dx[i] = __builtin_fmaf(-vv[i], s, g[i]);
       if (a.dsum) dx[i] += ds[i];
     }
-    T *o = static_cast<T *>(a.dx) + row * a.lddx;
-#pragma unroll
-    for (int k = 0; k < S::kVecs; ++k) {
-      const int c = S::col(k, t);
-      float q[VEC];
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) q[i] = dx[k * VEC + i];
-      if (c < n) store_n<VEC>(o + c, q);
-    }
+    S::template store<TAIL>(static_cast<T *>(a.dx) + row * a.lddx, dx, n, t);
     if constexpr (!kAhead) load_next();
   }
   if (!a.dweight) return;
@@ -392,12 +376,7 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void k_rms_norm_grad(
 #pragma unroll
       for (int i = 0; i < PER; ++i) dw[i] += sdw[q * S::kCols + i * 64 + t];
   }
-  float *o = part + (int64_t)blockIdx.x * n;
-#pragma unroll
-  for (int k = 0; k < S::kVecs; ++k)
-#pragma unroll
-    for (int i = 0; i < VEC; ++i)
-      if (S::col(k, t) < n) o[S::col(k, t) + i] = dw[k * VEC + i];
+  S::template store<TAIL>(part + (int64_t)blockIdx.x * n, dw, n, t);
 }
 
 // dx of one row per workgroup:
@@ -464,53 +443,39 @@ __global__ __launch_bounds__(1024) void k_rms_norm_dw_join(const float *__restri
 // ---------------------------------------------------------------- launchers
 static inline unsigned blocks_for(int64_t n, int per) { return (unsigned)((n + per - 1) / per); }
 
-// Whether rows of a matrix (null: none) start on multiples of `bytes`.
-static bool rows_aligned(const void *p, int64_t ld, size_t e, size_t bytes) {
-  return !p || (reinterpret_cast<uintptr_t>(p) % bytes == 0 && (size_t)ld * e % bytes == 0);
-}
-
-// The form of a row in registers by its length and alignment: calls f with T, VEC,
-// PER and WAVES as types; false where none holds it.
+// The form of a row in registers by its length: calls f with PER and WAVES as
+// types; false where none holds it.
 template <int N>
 using Int = std::integral_constant<int, N>;
-template <class T, class F>
-static bool by_row(int64_t cols, bool aligned, F f) {
-  constexpr int V = 16 / sizeof(T);
-  auto waves = [&](auto vec, auto w) {
-    constexpr int VEC = decltype(vec)::value, W = decltype(w)::value;
-    if (cols <= 8 * 64 * W)
-      f(vec, Int<8>(), w);
-    else
-      f(vec, Int<16>(), w);
-  };
-  auto row = [&](auto vec) {
-    if (cols <= 1024)
-      waves(vec, Int<1>());
-    else if (cols <= 4096)
-      waves(vec, Int<4>());
-    else
-      waves(vec, Int<16>());
-  };
-  if (cols > 16384) return false;
-  if (aligned && cols % V == 0)
-    row(Int<V>());
+template <bool deep, class F>
+static bool by_row(int64_t cols, F f) {
+  if (cols <= 512)
+    f(Int<8>(), Int<1>());
+  else if (cols <= 1024)
+    f(Int<16>(), Int<1>());
+  else if (cols <= 2048)
+    f(Int<deep ? 16 : 8>(), Int<deep ? 2 : 4>());
+  else if (cols <= 4096)
+    f(Int<deep ? 16 : 8>(), Int<deep ? 4 : 8>());
+  else if (cols <= 8192)
+    f(Int<deep ? 16 : 8>(), Int<deep ? 8 : 16>());
+  else if (cols <= 16384)
+    f(Int<16>(), Int<16>());
   else
-    row(Int<1>());
+    return false;
   return true;
 }
-constexpr int block_of(int waves) { return waves == 16 ? 1024 : 256; }
+constexpr int block_of(int waves) { return waves == 1 ? 256 : 64 * waves; }
 
 template <class T>
 static void run_rms_norm(const NormArgs &a, hipStream_t s) {
-  constexpr size_t e = sizeof(T);
-  const bool aligned = rows_aligned(a.x, a.ldx, e, 16) && rows_aligned(a.residual, a.ldr, e, 16) &&
-                       rows_aligned(a.sum, a.lds, e, 16) && rows_aligned(a.y, a.ldy, e, 16) &&
-                       rows_aligned(a.codes, a.ldc, 1, 8) && rows_aligned(a.weight, 0, 4, 16);
-  const bool done = by_row<T>(a.cols, aligned, [&](auto vec, auto per, auto w) {
+  auto go = [&](auto per, auto w) {
     constexpr int W = decltype(w)::value;
-    hipLaunchKernelGGL((k_rms_norm_reg<T, decltype(vec)::value, decltype(per)::value, W>),
-                       dim3(blocks_for(a.rows, block_of(W) / (64 * W))), dim3(block_of(W)), 0, s, a);
-  });
+    constexpr int VEC = 16 / sizeof(T), PER = decltype(per)::value;
+    auto kern = a.cols % VEC == 0 ? k_rms_norm_reg<T, VEC, PER, W, false> : k_rms_norm_reg<T, VEC, PER, W, true>;
+    hipLaunchKernelGGL(kern, dim3(blocks_for(a.rows, block_of(W) / (64 * W))), dim3(block_of(W)), 0, s, a);
+  };
+  const bool done = a.rows >= 512 ? by_row<true>(a.cols, go) : by_row<false>(a.cols, go);
   if (!done) hipLaunchKernelGGL(k_rms_norm<T>, dim3((unsigned)a.rows), dim3(256), 0, s, a);
 }
 hipError_t launch_rms_norm(int type, const NormArgs &a, hipStream_t s) {
@@ -534,15 +499,12 @@ size_t rms_norm_backward_ws(int64_t rows, int64_t cols) {
 
 template <class T>
 static void run_rms_norm_backward(const NormGradArgs &a, float *part, hipStream_t s) {
-  constexpr size_t e = sizeof(T);
   const int parts = grad_parts(a.rows);
-  const bool aligned = rows_aligned(a.dy, a.lddy, e, 16) && rows_aligned(a.v, a.ldv, e, 16) &&
-                       rows_aligned(a.dsum, a.ldds, e, 16) && rows_aligned(a.dx, a.lddx, e, 16) &&
-                       rows_aligned(a.weight, 0, 4, 16);
-  const bool done = by_row<T>(a.cols, aligned, [&](auto vec, auto per, auto w) {
+  const bool done = by_row<false>(a.cols, [&](auto per, auto w) {
     constexpr int W = decltype(w)::value;
-    hipLaunchKernelGGL((k_rms_norm_grad<T, decltype(vec)::value, decltype(per)::value, W>), dim3(parts),
-                       dim3(block_of(W)), 0, s, a, part);
+    constexpr int VEC = 16 / sizeof(T), PER = decltype(per)::value;
+    auto kern = a.cols % VEC == 0 ? k_rms_norm_grad<T, VEC, PER, W, false> : k_rms_norm_grad<T, VEC, PER, W, true>;
+    hipLaunchKernelGGL(kern, dim3(parts), dim3(block_of(W)), 0, s, a, part);
   });
   if (!done) {  // dweight first: dx may lie on an input
     if (a.dweight)
