@@ -12,7 +12,6 @@
 #include "ql_launch.h"
 
 #include <algorithm>
-#include <type_traits>
 
 namespace ql {
 
@@ -34,60 +33,6 @@ __device__ __forceinline__ F block_sum(F v, F *s) {
   return v;
 }
 
-// A row held by WAVES waves, PER values a thread in vectors of VEC: vector k of
-// thread t is values (k 64 WAVES + t) VEC .. + VEC - 1.
-template <int VEC, int PER, int WAVES>
-struct RowSlots {
-  static constexpr int kVecs = PER / VEC;
-  static constexpr int kThreads = 64 * WAVES;
-  static constexpr int kCols = PER * kThreads;  // the longest row
-  static __device__ __forceinline__ int col(int k, int t) { return (k * kThreads + t) * VEC; }
-  // The thread's values of a row of n, 0 past its end.  TAIL: n is no multiple of
-  // VEC; the one vector that the end cuts comes value by value, after the others
-  // are in flight.
-  template <bool TAIL, class T>
-  static __device__ __forceinline__ void load(float (&v)[PER], const T *p, int n, int t) {
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
-      const int c = col(k, t);
-      float q[VEC];
-      if (TAIL ? c + VEC <= n : c < n) {
-        load_n<VEC>(q, p + c);
-      } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) q[i] = 0.0f;
-      }
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) v[k * VEC + i] = q[i];
-    }
-    if constexpr (TAIL) {
-#pragma unroll
-      for (int k = 0; k < kVecs; ++k) {
-        const int c = col(k, t);
-        if (c < n && c + VEC > n)
-#pragma unroll
-          for (int i = 0; i < VEC - 1; ++i)
-            if (c + i < n) v[k * VEC + i] = (float)p[c + i];
-      }
-    }
-  }
-  template <bool TAIL, class T>
-  static __device__ __forceinline__ void store(T *p, const float (&v)[PER], int n, int t) {
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
-      const int c = col(k, t);
-      float q[VEC];
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) q[i] = v[k * VEC + i];
-      if (TAIL ? c + VEC <= n : c < n) store_n<VEC>(p + c, q);
-      if (TAIL && c < n && c + VEC > n)
-#pragma unroll
-        for (int i = 0; i < VEC - 1; ++i)
-          if (c + i < n) p[c + i] = (T)q[i];
-    }
-  }
-};
-
 }  // namespace
 
 // The row in registers: read once.  One wave per row up to 1024 values, four
@@ -97,8 +42,6 @@ __global__ __launch_bounds__((WAVES == 1 ? 256 : 64 * WAVES)) void k_rms_norm_re
   typedef RowSlots<VEC, PER, WAVES> S;
   constexpr int kBlock = (WAVES == 1 ? 256 : 64 * WAVES), kRows = kBlock / S::kThreads;
   __shared__ double ssum[16];
-  __shared__ float slo[16], shi[16];
-  __shared__ int sbad[16], scodes[16];
   const int t = threadIdx.x % S::kThreads, wave = threadIdx.x >> 6;
   const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / S::kThreads;
   if (WAVES == 1 && row >= a.rows) return;  // (no barriers in this form)
@@ -140,75 +83,8 @@ __global__ __launch_bounds__((WAVES == 1 ? 256 : 64 * WAVES)) void k_rms_norm_re
   }
   if (a.y) S::template store<TAIL>(static_cast<T *>(a.y) + row * a.ldy, v, n, t);
   if (!a.codes) return;
-  float lo = INFINITY, hi = -INFINITY, nan = 0.0f;
-#pragma unroll
-  for (int e = 0; e < PER; ++e)
-    if (S::col(e / VEC, t) + e % VEC < n) {
-      lo = fminf(lo, v[e]);
-      hi = fmaxf(hi, v[e]);
-      nan = __builtin_fmaf(v[e], 0.0f, nan);  // NaN where one is not finite
-    }
-  lo = wave_min(lo);
-  hi = wave_max(hi);
-  bool bad = __any(nan != nan);
-  if constexpr (WAVES > 1) {
-    if ((threadIdx.x & 63) == 0) slo[wave] = lo, shi[wave] = hi, sbad[wave] = bad;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      lo = fminf(lo, slo[w]);
-      hi = fmaxf(hi, shi[w]);
-      bad |= sbad[w] != 0;
-    }
-  }
-  // a row with a value that is not finite: every code 0 (Q = 0, z = 0)
-  const QParams p = bad ? QParams{0.0, 0, __builtin_nanf(""), 0.0} : make_qparams(lo, hi);
-  const FastEncode f = bad ? FastEncode{0.0f, 0.0f, 2.0f} : fast_encode(p, lo, hi);
-  int8_t *o = a.codes + row * a.ldc;
-  uint32_t codesum = 0;
-#pragma unroll
-  for (int k = 0; k < S::kVecs; ++k) {
-    const int c = S::col(k, t);
-    float q[VEC];
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) q[i] = bad ? 0.0f : v[k * VEC + i];
-    uint32_t w[VEC / 4];
-    encode_words<VEC>(q, p, f, w);
-    if (TAIL ? c + VEC <= n : c < n) {
-      typedef uint32_t vec __attribute__((ext_vector_type(VEC / 4)));
-      typedef vec any __attribute__((aligned(1)));
-      vec o4;
-#pragma unroll
-      for (int i = 0; i < VEC / 4; ++i) {
-        codesum = add_codes(w[i], codesum);
-        o4[i] = w[i] ^ 0x80808080u;
-      }
-      *reinterpret_cast<any *>(o + c) = o4;
-    } else if (TAIL) {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i)
-        if (c + i < n) {
-          const uint32_t code = (w[i / 4] >> (8 * (i % 4))) & 255u;
-          codesum += code;
-          o[c + i] = (int8_t)(code ^ 0x80u);
-        }
-    }
-  }
-  int sum = (int)codesum;
-  for (int64_t c = n + t; c < a.ldc; c += S::kThreads) o[c] = 0;
-  sum = wave_sum(sum);
-  if constexpr (WAVES > 1) {
-    if ((threadIdx.x & 63) == 0) scodes[wave] = sum;
-    __syncthreads();
-    sum = scodes[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) sum += scodes[w];
-  }
-  if (t == 0) {
-    a.zero[row] = p.z;
-    a.inv_q[row] = p.inv_q;
-    a.sums[row] = sum;
-  }
+  code_row<VEC, PER, WAVES, TAIL>(v, n, t, a.codes + row * a.ldc, a.ldc, a.zero + row,
+                                  a.inv_q + row, a.sums + row);
 }
 
 // One workgroup per row, the row read three times (sum of squares, range, result);
@@ -442,30 +318,6 @@ __global__ __launch_bounds__(1024) void k_rms_norm_dw_join(const float *__restri
 
 // ---------------------------------------------------------------- launchers
 static inline unsigned blocks_for(int64_t n, int per) { return (unsigned)((n + per - 1) / per); }
-
-// The form of a row in registers by its length: calls f with PER and WAVES as
-// types; false where none holds it.
-template <int N>
-using Int = std::integral_constant<int, N>;
-template <bool deep, class F>
-static bool by_row(int64_t cols, F f) {
-  if (cols <= 512)
-    f(Int<8>(), Int<1>());
-  else if (cols <= 1024)
-    f(Int<16>(), Int<1>());
-  else if (cols <= 2048)
-    f(Int<deep ? 16 : 8>(), Int<deep ? 2 : 4>());
-  else if (cols <= 4096)
-    f(Int<deep ? 16 : 8>(), Int<deep ? 4 : 8>());
-  else if (cols <= 8192)
-    f(Int<deep ? 16 : 8>(), Int<deep ? 8 : 16>());
-  else if (cols <= 16384)
-    f(Int<16>(), Int<16>());
-  else
-    return false;
-  return true;
-}
-constexpr int block_of(int waves) { return waves == 1 ? 256 : 64 * waves; }
 
 template <class T>
 static void run_rms_norm(const NormArgs &a, hipStream_t s) {

@@ -128,110 +128,210 @@ __global__ __launch_bounds__(256) void k_quantize_rows_of(const T *__restrict__ 
   }
 }
 
-// The product.  A wave takes 16 rows of W (lane: row r = lane & 15, share
+// A row of any type in registers (as the norm holds it), quantized.
+template <class T, int VEC, int PER, int WAVES, bool TAIL>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_quantize_rows_reg(
+    const T *__restrict__ X, int64_t ldx, int64_t m, int n, int8_t *__restrict__ codes, int64_t ld,
+    int32_t *__restrict__ zero, float *__restrict__ inv_q, int32_t *__restrict__ sums) {
+  typedef RowSlots<VEC, PER, WAVES> S;
+  constexpr int kRows = (WAVES == 1 ? 256 : 64 * WAVES) / S::kThreads;
+  const int t = threadIdx.x % S::kThreads;
+  const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / S::kThreads;
+  if (WAVES == 1 && row >= m) return;  // (no barriers in this form)
+  float v[PER];
+  S::template load<TAIL>(v, X + row * ldx, n, t);
+  code_row<VEC, PER, WAVES, TAIL>(v, n, t, codes + row * ld, ld, zero + row, inv_q + row, sums + row);
+}
+
+// The product.  A wave takes 16 NT rows of W (lane: row r = lane & 15 of 16, share
 // q = lane >> 4 of the columns) and 16 MT rows of X.  Per group three products
 // on the matrix units: W X (16 sum c x), W 1 (16 sum c) and 1 X (sum x), with
 // c = V' - 8 and x = x' - 128; then, with z = z_g + 8 and zt = zx + 128,
-//   16 T_g = W X + 16 z (1 X) + zt (W 1 + 16 z G)
-// in fp32: every term but the last fma's result is an integer below 2^24.
-template <int G, int MT, class TY>
-__global__ __launch_bounds__(256) void k_matmul4(Q4Mat W, ActRows X, int64_t M, int64_t ncols,
-                                                 const float *__restrict__ bias,
-                                                 TY *__restrict__ Y) {
-  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
-  const int64_t n0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 16;
-  const int64_t m0 = (int64_t)blockIdx.y * 16 * MT;
-  if (n0 >= W.rows) return;
-  const uint8_t *w = W.codes + (n0 + r < W.rows ? n0 + r : W.rows - 1) * (W.ld / 2) + 16 * q;
-  const int8_t *x[MT];
-  float zt[MT];
-#pragma unroll
-  for (int b = 0; b < MT; ++b) {
-    const int64_t m = m0 + 16 * b + r < M ? m0 + 16 * b + r : M - 1;
-    x[b] = X.codes + m * X.ld;
-    zt[b] = (float)(X.zero[m] + 128);
-  }
-  float acc[MT][4];
-#pragma unroll
-  for (int b = 0; b < MT; ++b)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc[b][i] = 0.0f;
+//   16 T_g = W X + [16 z, W 1 + 16 z G] . [1 X, zt]
+// is one 16-bit dot product onto the first's result, exact; one conversion and one
+// fma per group follow.  (Rows whose range lies so far off 0 that zt does not
+// fit 16 bits: the same in fp32, every term an integer below 2^24 but the last.)
+//
+// The columns are split over the waves of a workgroup, `per` runs of 128 each, and
+// their sums added in order: a function of the matrix alone, so that a row's
+// result does not depend on the rows beside it.  The waves' weights are read
+// once, straight into registers; codes of X come through the caches, which the
+// workgroups share.
+template <int G, int MT, int NT, bool WIDE>
+__device__ __forceinline__ void mul4_runs(const Q4Mat &W, const uint8_t *const (&w)[NT],
+                                          const int8_t *const (&x)[MT], int64_t ldx,
+                                          const int (&zx)[MT], int64_t n0, int q, int64_t k0,
+                                          int64_t k1, float (&acc)[NT][MT][4]) {
+  constexpr int kParts = 128 / G;     // groups in a run
+  constexpr int kWords = 4 / kParts;  // words of a lane in a group
   const v4i one{0x01010101, 0x01010101, 0x01010101, 0x01010101};
-  const int64_t runs = W.ld / 128;
-  for (int64_t k = 0; k < runs; ++k) {
-    const uint4 wv = *reinterpret_cast<const uint4 *>(w + 64 * k);
-    const uint32_t ww[4] = {wv.x, wv.y, wv.z, wv.w};
+  typedef short v2s __attribute__((ext_vector_type(2)));
+  for (int64_t k = k0; k < k1; ++k) {
+    uint32_t ww[NT][4];
     int2 xv[MT][4];
+    float4 qv[kParts][NT];
+    int zv[kParts][NT];
+#pragma unroll
+    for (int a = 0; a < NT; ++a) {
+      const uint4 v = *reinterpret_cast<const uint4 *>(w[a] + 64 * k);
+      ww[a][0] = v.x, ww[a][1] = v.y, ww[a][2] = v.z, ww[a][3] = v.w;
+    }
 #pragma unroll
     for (int b = 0; b < MT; ++b)
 #pragma unroll
       for (int p = 0; p < 4; ++p) {
-        // columns at and past X.ld recover to 0 in W: any codes serve
+        // columns at and past ldx recover to 0 in W: any codes serve
         const int64_t c = 128 * k + 32 * p + 8 * q;
-        xv[b][p] = *reinterpret_cast<const int2 *>(x[b] + (c < X.ld ? c : 0));
+        xv[b][p] = *reinterpret_cast<const int2 *>(x[b] + (c < ldx ? c : 0));
       }
-    constexpr int kParts = 128 / G;   // groups in a run
-    constexpr int kWords = 4 / kParts;  // words of a lane in a group
+#pragma unroll
+    for (int gp = 0; gp < kParts; ++gp)
+#pragma unroll
+      for (int a = 0; a < NT; ++a) {
+        const int64_t at = (k * kParts + gp) * W.ldr + n0 + 16 * a + 4 * q;
+        qv[gp][a] = *reinterpret_cast<const float4 *>(W.inv_q + at);
+        zv[gp][a] = *reinterpret_cast<const int *>(W.zero + at);
+      }
 #pragma unroll
     for (int gp = 0; gp < kParts; ++gp) {
-      const int64_t g = k * kParts + gp;
-      const float4 qv = *reinterpret_cast<const float4 *>(W.inv_q + g * W.ldr + n0 + 4 * q);
-      const int zv = *reinterpret_cast<const int *>(W.zero + g * W.ldr + n0 + 4 * q);
-      v4i wx[MT], w1{}, x1[MT];
+      v4i wx[NT][MT], w1[NT], x1[MT];
 #pragma unroll
-      for (int b = 0; b < MT; ++b) wx[b] = v4i{}, x1[b] = v4i{};
+      for (int a = 0; a < NT; ++a) {
+        w1[a] = v4i{};
+#pragma unroll
+        for (int b = 0; b < MT; ++b) wx[a][b] = v4i{};
+      }
+#pragma unroll
+      for (int b = 0; b < MT; ++b) x1[b] = v4i{};
       if constexpr (kWords >= 2) {
 #pragma unroll
         for (int h = 0; h < kWords / 2; ++h) {
           const int p = gp * kWords + 2 * h;
-          const v4i a{(int)((ww[p] << 4) & kHigh), (int)(ww[p] & kHigh),
-                      (int)((ww[p + 1] << 4) & kHigh), (int)(ww[p + 1] & kHigh)};
-          w1 = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, one, w1, 0, 0, 0);
+          v4i bx[MT];
 #pragma unroll
           for (int b = 0; b < MT; ++b) {
-            const v4i bx{xv[b][p].x, xv[b][p].y, xv[b][p + 1].x, xv[b][p + 1].y};
-            wx[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, bx, wx[b], 0, 0, 0);
-            x1[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(one, bx, x1[b], 0, 0, 0);
+            bx[b] = v4i{xv[b][p].x, xv[b][p].y, xv[b][p + 1].x, xv[b][p + 1].y};
+            x1[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(one, bx[b], x1[b], 0, 0, 0);
+          }
+#pragma unroll
+          for (int a = 0; a < NT; ++a) {
+            const v4i wa{(int)((ww[a][p] << 4) & kHigh), (int)(ww[a][p] & kHigh),
+                         (int)((ww[a][p + 1] << 4) & kHigh), (int)(ww[a][p + 1] & kHigh)};
+            w1[a] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wa, one, w1[a], 0, 0, 0);
+#pragma unroll
+            for (int b = 0; b < MT; ++b)
+              wx[a][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wa, bx[b], wx[a][b], 0, 0, 0);
           }
         }
       } else {
         auto pair = [](uint32_t lo, uint32_t hi) { return (long)(((uint64_t)hi << 32) | lo); };
-        const long a = pair((ww[gp] << 4) & kHigh, ww[gp] & kHigh);
         const long one8 = 0x0101010101010101l;
-        w1 = __builtin_amdgcn_mfma_i32_16x16x32_i8(a, one8, w1, 0, 0, 0);
+        long bx[MT];
 #pragma unroll
         for (int b = 0; b < MT; ++b) {
-          const long bx = pair((uint32_t)xv[b][gp].x, (uint32_t)xv[b][gp].y);
-          wx[b] = __builtin_amdgcn_mfma_i32_16x16x32_i8(a, bx, wx[b], 0, 0, 0);
-          x1[b] = __builtin_amdgcn_mfma_i32_16x16x32_i8(one8, bx, x1[b], 0, 0, 0);
+          bx[b] = pair((uint32_t)xv[b][gp].x, (uint32_t)xv[b][gp].y);
+          x1[b] = __builtin_amdgcn_mfma_i32_16x16x32_i8(one8, bx[b], x1[b], 0, 0, 0);
+        }
+#pragma unroll
+        for (int a = 0; a < NT; ++a) {
+          const long wa = pair((ww[a][gp] << 4) & kHigh, ww[a][gp] & kHigh);
+          w1[a] = __builtin_amdgcn_mfma_i32_16x16x32_i8(wa, one8, w1[a], 0, 0, 0);
+#pragma unroll
+          for (int b = 0; b < MT; ++b)
+            wx[a][b] = __builtin_amdgcn_mfma_i32_16x16x32_i8(wa, bx[b], wx[a][b], 0, 0, 0);
         }
       }
-      const float qs[4] = {qv.x, qv.y, qv.z, qv.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float z16 = (float)(16 * ((int)(int8_t)(zv >> (8 * i)) + 8));
-        const float ws = __builtin_fmaf(z16, (float)G, (float)w1[i]);
+      for (int a = 0; a < NT; ++a) {
+        const float qs[4] = {qv[gp][a].x, qv[gp][a].y, qv[gp][a].z, qv[gp][a].w};
 #pragma unroll
-        for (int b = 0; b < MT; ++b) {
-          const float t = __builtin_fmaf(z16, (float)x1[b][i], (float)wx[b][i]);
-          acc[b][i] = __builtin_fmaf(qs[i], __builtin_fmaf(zt[b], ws, t), acc[b][i]);
+        for (int i = 0; i < 4; ++i) {
+          const int z16 = 16 * ((int)(int8_t)(zv[gp][a] >> (8 * i)) + 8);
+          const int ws = w1[a][i] + z16 * G;
+#pragma unroll
+          for (int b = 0; b < MT; ++b) {
+            // (every row of 1 X is alike)
+            float t;
+            if constexpr (WIDE) {
+              t = __builtin_fmaf((float)z16, (float)x1[b][0], (float)wx[a][b][i]);
+              t = __builtin_fmaf((float)zx[b], (float)ws, t);
+            } else {
+              const v2s u{(short)z16, (short)ws}, v{(short)x1[b][0], (short)zx[b]};
+              t = (float)__builtin_amdgcn_sdot2(u, v, wx[a][b][i], false);
+            }
+            acc[a][b][i] = __builtin_fmaf(qs[i], t, acc[a][b][i]);
+          }
         }
       }
     }
   }
+}
+
+constexpr int kSlices = 8;  // waves that the columns are split over, at most
+template <int G, int MT, int NT, class TY>
+__global__ __launch_bounds__(64 * kSlices) void k_matmul4(Q4Mat W, ActRows X, int64_t M, int per,
+                                                          const float *__restrict__ bias,
+                                                          TY *__restrict__ Y) {
+  extern __shared__ float4 parts[];  // [waves][NT MT][64]
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
+  const int waves = blockDim.x >> 6;
+  const int64_t n0 = (int64_t)blockIdx.x * 16 * NT, m0 = (int64_t)blockIdx.y * 16 * MT;
+  const uint8_t *w[NT];
+#pragma unroll
+  for (int a = 0; a < NT; ++a) {
+    const int64_t n = n0 + 16 * a + r;
+    w[a] = W.codes + (n < W.rows ? n : W.rows - 1) * (W.ld / 2) + 16 * q;
+  }
+  const int8_t *x[MT];
+  int zx[MT];
+  bool wide = false;
 #pragma unroll
   for (int b = 0; b < MT; ++b) {
-    const int64_t m = m0 + 16 * b + r;
-    if (m >= M) continue;
-    const float qx = X.inv_q[m] * 0.0625f;
+    const int64_t m = m0 + 16 * b + r < M ? m0 + 16 * b + r : M - 1;
+    x[b] = X.codes + m * X.ld;
+    zx[b] = X.zero[m] + 128;
+    wide |= zx[b] != (int)(short)zx[b];
+  }
+  float acc[NT][MT][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t n = n0 + 4 * q + i;
-      if (n < ncols) {
-        float y = acc[b][i] * qx;
-        if (bias) y += bias[n];
-        Y[m * ncols + n] = (TY)y;
-      }
+  for (int a = 0; a < NT; ++a)
+#pragma unroll
+    for (int b = 0; b < MT; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[a][b][i] = 0.0f;
+  const int64_t runs = W.ld / 128, k0 = (int64_t)wave * per, k1 = k0 + per < runs ? k0 + per : runs;
+  if (__any(wide))
+    mul4_runs<G, MT, NT, true>(W, w, x, X.ld, zx, n0, q, k0, k1, acc);
+  else
+    mul4_runs<G, MT, NT, false>(W, w, x, X.ld, zx, n0, q, k0, k1, acc);
+  // the waves' sums, added in order
+#pragma unroll
+  for (int a = 0; a < NT; ++a)
+#pragma unroll
+    for (int b = 0; b < MT; ++b)
+      parts[(wave * NT * MT + a * MT + b) * 64 + lane] =
+          make_float4(acc[a][b][0], acc[a][b][1], acc[a][b][2], acc[a][b][3]);
+  __syncthreads();
+  for (int tile = wave; tile < NT * MT; tile += waves) {
+    const int64_t n = n0 + 16 * (tile / MT) + 4 * q, m = m0 + 16 * (tile % MT) + r;
+    if (n >= W.rows || m >= M) continue;
+    float4 s = parts[tile * 64 + lane];
+    for (int p = 1; p < waves; ++p) {
+      const float4 v = parts[(p * NT * MT + tile) * 64 + lane];
+      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    }
+    const float qx = X.inv_q[m] * 0.0625f;
+    float y[4] = {s.x * qx, s.y * qx, s.z * qx, s.w * qx};
+    TY *o = Y + m * W.rows + n;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (bias && n + i < W.rows) y[i] += bias[n + i];
+    if (n + 4 <= W.rows) {
+      store_n<4>(o, y);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (n + i < W.rows) o[i] = (TY)y[i];
     }
   }
 }
@@ -253,41 +353,58 @@ hipError_t launch_dequantize4(const Q4Mat &q, int64_t cols, float *dst, hipStrea
   return hipGetLastError();
 }
 
+template <class T>
+static void run_quantize_rows(const T *X, int64_t ldx, int64_t m, int64_t K, int8_t *codes,
+                              int64_t ld, int32_t *zero, float *inv_q, int32_t *sums,
+                              hipStream_t s) {
+  auto go = [&](auto per, auto w) {
+    constexpr int W = decltype(w)::value, VEC = 16 / sizeof(T), PER = decltype(per)::value;
+    auto kern = K % VEC == 0 ? k_quantize_rows_reg<T, VEC, PER, W, false>
+                             : k_quantize_rows_reg<T, VEC, PER, W, true>;
+    hipLaunchKernelGGL(kern, dim3(blocks_for(m, block_of(W) / (64 * W))), dim3(block_of(W)), 0, s, X,
+                       ldx, m, (int)K, codes, ld, zero, inv_q, sums);
+  };
+  const bool done = m >= 512 ? by_row<true>(K, go) : by_row<false>(K, go);
+  if (!done)
+    hipLaunchKernelGGL(k_quantize_rows_of<T>, dim3(blocks_for(m, 4)), dim3(256), 0, s, X, ldx, m, K,
+                       codes, ld, zero, inv_q, sums);
+}
 hipError_t launch_quantize_rows_of(int type, const void *X, int64_t ldx, int64_t m, int64_t K,
                                    int8_t *codes, int64_t ld, int32_t *zero, float *inv_q,
                                    int32_t *sums, hipStream_t s) {
   if (m == 0) return hipSuccess;
-  const dim3 grid(blocks_for(m, 4)), block(256);
   if (type == 0)
-    hipLaunchKernelGGL(k_quantize_rows_of<float>, grid, block, 0, s, static_cast<const float *>(X),
-                       ldx, m, K, codes, ld, zero, inv_q, sums);
+    run_quantize_rows(static_cast<const float *>(X), ldx, m, K, codes, ld, zero, inv_q, sums, s);
   else if (type == 1)
-    hipLaunchKernelGGL(k_quantize_rows_of<f16>, grid, block, 0, s, static_cast<const f16 *>(X), ldx,
-                       m, K, codes, ld, zero, inv_q, sums);
+    run_quantize_rows(static_cast<const f16 *>(X), ldx, m, K, codes, ld, zero, inv_q, sums, s);
   else
-    hipLaunchKernelGGL(k_quantize_rows_of<bf16>, grid, block, 0, s, static_cast<const bf16 *>(X),
-                       ldx, m, K, codes, ld, zero, inv_q, sums);
+    run_quantize_rows(static_cast<const bf16 *>(X), ldx, m, K, codes, ld, zero, inv_q, sums, s);
   return hipGetLastError();
 }
 
-template <int MT, class TY>
+template <int MT, int NT, class TY>
 static void run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, TY *Y,
                         hipStream_t s) {
-  const dim3 grid(blocks_for(W.rows, 64), blocks_for(M, 16 * MT));
-  auto kern = W.group == 32 ? k_matmul4<32, MT, TY>
-              : W.group == 64 ? k_matmul4<64, MT, TY>
-                              : k_matmul4<128, MT, TY>;
-  hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, W, X, M, W.rows, bias, Y);
+  const int runs = (int)(W.ld / 128);
+  int waves = 1;
+  while (waves < kSlices && 2 * waves <= runs) waves *= 2;
+  const int per = (runs + waves - 1) / waves;
+  const dim3 grid(blocks_for(W.rows, 16 * NT), blocks_for(M, 16 * MT));
+  auto kern = W.group == 32 ? k_matmul4<32, MT, NT, TY>
+              : W.group == 64 ? k_matmul4<64, MT, NT, TY>
+                              : k_matmul4<128, MT, NT, TY>;
+  hipLaunchKernelGGL(kern, grid, dim3(64 * waves), waves * NT * MT * 64 * sizeof(float4), s, W, X, M,
+                     per, bias, Y);
 }
 template <class TY>
 static void run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, TY *Y,
                         hipStream_t s) {
   if (M <= 16)
-    run_matmul4<1, TY>(W, X, M, bias, Y, s);
+    run_matmul4<1, 1, TY>(W, X, M, bias, Y, s);
   else if (M <= 32)
-    run_matmul4<2, TY>(W, X, M, bias, Y, s);
+    run_matmul4<2, 2, TY>(W, X, M, bias, Y, s);
   else
-    run_matmul4<4, TY>(W, X, M, bias, Y, s);
+    run_matmul4<4, 2, TY>(W, X, M, bias, Y, s);
 }
 hipError_t launch_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, int ytype,
                           void *Y, hipStream_t s) {
