@@ -19,6 +19,8 @@
 #include "ql_elem.h"
 #include "ql_launch.h"
 
+#include <algorithm>
+
 namespace ql {
 
 constexpr uint32_t kHigh = 0xf0f0f0f0u;
@@ -152,187 +154,336 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_quantize_rows
 // fma per group follow.  (Rows whose range lies so far off 0 that zt does not
 // fit 16 bits: the same in fp32, every term an integer below 2^24 but the last.)
 //
-// The columns are split over the waves of a workgroup, `per` runs of 128 each, and
-// their sums added in order: a function of the matrix alone, so that a row's
-// result does not depend on the rows beside it.  The waves' weights are read
-// once, straight into registers; codes of X come through the caches, which the
-// workgroups share.
-template <int G, int MT, int NT, bool WIDE>
-__device__ __forceinline__ void mul4_runs(const Q4Mat &W, const uint8_t *const (&w)[NT],
-                                          const int8_t *const (&x)[MT], int64_t ldx,
-                                          const int (&zx)[MT], int64_t n0, int q, int64_t k0,
-                                          int64_t k1, float (&acc)[NT][MT][4]) {
-  constexpr int kParts = 128 / G;     // groups in a run
-  constexpr int kWords = 4 / kParts;  // words of a lane in a group
-  const v4i one{0x01010101, 0x01010101, 0x01010101, 0x01010101};
-  typedef short v2s __attribute__((ext_vector_type(2)));
-  for (int64_t k = k0; k < k1; ++k) {
-    uint32_t ww[NT][4];
-    int2 xv[MT][4];
-    float4 qv[kParts][NT];
-    int zv[kParts][NT];
-#pragma unroll
-    for (int a = 0; a < NT; ++a) {
-      const uint4 v = *reinterpret_cast<const uint4 *>(w[a] + 64 * k);
-      ww[a][0] = v.x, ww[a][1] = v.y, ww[a][2] = v.z, ww[a][3] = v.w;
-    }
-#pragma unroll
-    for (int b = 0; b < MT; ++b)
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        // columns at and past ldx recover to 0 in W: any codes serve
-        const int64_t c = 128 * k + 32 * p + 8 * q;
-        xv[b][p] = *reinterpret_cast<const int2 *>(x[b] + (c < ldx ? c : 0));
-      }
+// The columns are cut into slices that the waves of a workgroup share, and the
+// slices' sums added in an order that depends on the matrix alone: a row's result
+// does not depend on the rows beside it.
+// One run's scales and zero points of the lane's 4 NT output rows.
+template <int G, int NT>
+struct RunScales {
+  static constexpr int kParts = 128 / G;  // groups in a run
+  float4 q[kParts][NT];
+  int z[kParts][NT];
+  __device__ __forceinline__ void load(const Q4Mat &W, int64_t k, int64_t n) {
 #pragma unroll
     for (int gp = 0; gp < kParts; ++gp)
 #pragma unroll
       for (int a = 0; a < NT; ++a) {
-        const int64_t at = (k * kParts + gp) * W.ldr + n0 + 16 * a + 4 * q;
-        qv[gp][a] = *reinterpret_cast<const float4 *>(W.inv_q + at);
-        zv[gp][a] = *reinterpret_cast<const int *>(W.zero + at);
+        const int64_t at = (k * kParts + gp) * W.ldr + n + 16 * a;
+        q[gp][a] = *reinterpret_cast<const float4 *>(W.inv_q + at);
+        z[gp][a] = *reinterpret_cast<const int *>(W.zero + at);
       }
+  }
+};
+// One run: the lane's 16 bytes of each 16 rows of W against its codes of X, four
+// 8-byte pieces (32 columns apart) of each 16 rows.
+template <int G, int MT, int NT, bool WIDE>
+__device__ __forceinline__ void mul4_run(const uint4 (&wv)[NT], const int2 (&xv)[MT][4],
+                                         const RunScales<G, NT> &sc, const int (&zx)[MT],
+                                         float (&acc)[NT][MT][4]) {
+  constexpr int kParts = 128 / G;
+  constexpr int kWords = 4 / kParts;  // words of a lane in a group
+  const v4i one{0x01010101, 0x01010101, 0x01010101, 0x01010101};
+  typedef short v2s __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int gp = 0; gp < kParts; ++gp) {
-      v4i wx[NT][MT], w1[NT], x1[MT];
+  for (int gp = 0; gp < kParts; ++gp) {
+    v4i x1[MT];
 #pragma unroll
-      for (int a = 0; a < NT; ++a) {
-        w1[a] = v4i{};
+    for (int b = 0; b < MT; ++b) x1[b] = v4i{};
+    auto pair = [](uint32_t lo, uint32_t hi) { return (long)(((uint64_t)hi << 32) | lo); };
+    const long one8 = 0x0101010101010101l;
 #pragma unroll
-        for (int b = 0; b < MT; ++b) wx[a][b] = v4i{};
-      }
-#pragma unroll
-      for (int b = 0; b < MT; ++b) x1[b] = v4i{};
+    for (int b = 0; b < MT; ++b) {
       if constexpr (kWords >= 2) {
 #pragma unroll
-        for (int h = 0; h < kWords / 2; ++h) {
-          const int p = gp * kWords + 2 * h;
-          v4i bx[MT];
-#pragma unroll
-          for (int b = 0; b < MT; ++b) {
-            bx[b] = v4i{xv[b][p].x, xv[b][p].y, xv[b][p + 1].x, xv[b][p + 1].y};
-            x1[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(one, bx[b], x1[b], 0, 0, 0);
-          }
-#pragma unroll
-          for (int a = 0; a < NT; ++a) {
-            const v4i wa{(int)((ww[a][p] << 4) & kHigh), (int)(ww[a][p] & kHigh),
-                         (int)((ww[a][p + 1] << 4) & kHigh), (int)(ww[a][p + 1] & kHigh)};
-            w1[a] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wa, one, w1[a], 0, 0, 0);
-#pragma unroll
-            for (int b = 0; b < MT; ++b)
-              wx[a][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wa, bx[b], wx[a][b], 0, 0, 0);
-          }
-        }
+        for (int p = gp * kWords; p < (gp + 1) * kWords; p += 2)
+          x1[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+              one, v4i{xv[b][p].x, xv[b][p].y, xv[b][p + 1].x, xv[b][p + 1].y}, x1[b], 0, 0, 0);
       } else {
-        auto pair = [](uint32_t lo, uint32_t hi) { return (long)(((uint64_t)hi << 32) | lo); };
-        const long one8 = 0x0101010101010101l;
-        long bx[MT];
+        x1[b] = __builtin_amdgcn_mfma_i32_16x16x32_i8(
+            one8, pair((uint32_t)xv[b][gp].x, (uint32_t)xv[b][gp].y), x1[b], 0, 0, 0);
+      }
+    }
 #pragma unroll
-        for (int b = 0; b < MT; ++b) {
-          bx[b] = pair((uint32_t)xv[b][gp].x, (uint32_t)xv[b][gp].y);
-          x1[b] = __builtin_amdgcn_mfma_i32_16x16x32_i8(one8, bx[b], x1[b], 0, 0, 0);
-        }
+    for (int a = 0; a < NT; ++a) {
+      const uint32_t ww[4] = {wv[a].x, wv[a].y, wv[a].z, wv[a].w};
+      v4i wx[MT], w1{};
 #pragma unroll
-        for (int a = 0; a < NT; ++a) {
-          const long wa = pair((ww[a][gp] << 4) & kHigh, ww[a][gp] & kHigh);
-          w1[a] = __builtin_amdgcn_mfma_i32_16x16x32_i8(wa, one8, w1[a], 0, 0, 0);
+      for (int b = 0; b < MT; ++b) wx[b] = v4i{};
+      if constexpr (kWords >= 2) {
+#pragma unroll
+        for (int p = gp * kWords; p < (gp + 1) * kWords; p += 2) {
+          const v4i wa{(int)((ww[p] << 4) & kHigh), (int)(ww[p] & kHigh),
+                       (int)((ww[p + 1] << 4) & kHigh), (int)(ww[p + 1] & kHigh)};
+          w1 = __builtin_amdgcn_mfma_i32_16x16x64_i8(wa, one, w1, 0, 0, 0);
 #pragma unroll
           for (int b = 0; b < MT; ++b)
-            wx[a][b] = __builtin_amdgcn_mfma_i32_16x16x32_i8(wa, bx[b], wx[a][b], 0, 0, 0);
+            wx[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+                wa, v4i{xv[b][p].x, xv[b][p].y, xv[b][p + 1].x, xv[b][p + 1].y}, wx[b], 0, 0, 0);
         }
+      } else {
+        const long wa = pair((ww[gp] << 4) & kHigh, ww[gp] & kHigh);
+        w1 = __builtin_amdgcn_mfma_i32_16x16x32_i8(wa, one8, w1, 0, 0, 0);
+#pragma unroll
+        for (int b = 0; b < MT; ++b)
+          wx[b] = __builtin_amdgcn_mfma_i32_16x16x32_i8(
+              wa, pair((uint32_t)xv[b][gp].x, (uint32_t)xv[b][gp].y), wx[b], 0, 0, 0);
       }
+      const float qs[4] = {sc.q[gp][a].x, sc.q[gp][a].y, sc.q[gp][a].z, sc.q[gp][a].w};
 #pragma unroll
-      for (int a = 0; a < NT; ++a) {
-        const float qs[4] = {qv[gp][a].x, qv[gp][a].y, qv[gp][a].z, qv[gp][a].w};
+      for (int i = 0; i < 4; ++i) {
+        const int z16 = 16 * ((int)(int8_t)(sc.z[gp][a] >> (8 * i)) + 8);
+        const int ws = w1[i] + z16 * G;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int z16 = 16 * ((int)(int8_t)(zv[gp][a] >> (8 * i)) + 8);
-          const int ws = w1[a][i] + z16 * G;
-#pragma unroll
-          for (int b = 0; b < MT; ++b) {
-            // (every row of 1 X is alike)
-            float t;
-            if constexpr (WIDE) {
-              t = __builtin_fmaf((float)z16, (float)x1[b][0], (float)wx[a][b][i]);
-              t = __builtin_fmaf((float)zx[b], (float)ws, t);
-            } else {
-              const v2s u{(short)z16, (short)ws}, v{(short)x1[b][0], (short)zx[b]};
-              t = (float)__builtin_amdgcn_sdot2(u, v, wx[a][b][i], false);
-            }
-            acc[a][b][i] = __builtin_fmaf(qs[i], t, acc[a][b][i]);
+        for (int b = 0; b < MT; ++b) {
+          // (every row of 1 X is alike)
+          float t;
+          if constexpr (WIDE) {
+            t = __builtin_fmaf((float)z16, (float)x1[b][0], (float)wx[b][i]);
+            t = __builtin_fmaf((float)zx[b], (float)ws, t);
+          } else {
+            const v2s u{(short)z16, (short)ws}, v{(short)x1[b][0], (short)zx[b]};
+            t = (float)__builtin_amdgcn_sdot2(u, v, wx[b][i], false);
           }
+          acc[a][b][i] = __builtin_fmaf(qs[i], t, acc[a][b][i]);
         }
       }
     }
   }
 }
 
-constexpr int kSlices = 8;  // waves that the columns are split over, at most
-template <int G, int MT, int NT, class TY>
-__global__ __launch_bounds__(64 * kSlices) void k_matmul4(Q4Mat W, ActRows X, int64_t M, int per,
-                                                          const float *__restrict__ bias,
-                                                          TY *__restrict__ Y) {
-  extern __shared__ float4 parts[];  // [waves][NT MT][64]
-  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
-  const int waves = blockDim.x >> 6;
-  const int64_t n0 = (int64_t)blockIdx.x * 16 * NT, m0 = (int64_t)blockIdx.y * 16 * MT;
-  const uint8_t *w[NT];
-#pragma unroll
-  for (int a = 0; a < NT; ++a) {
-    const int64_t n = n0 + 16 * a + r;
-    w[a] = W.codes + (n < W.rows ? n : W.rows - 1) * (W.ld / 2) + 16 * q;
-  }
-  const int8_t *x[MT];
-  int zx[MT];
-  bool wide = false;
-#pragma unroll
-  for (int b = 0; b < MT; ++b) {
-    const int64_t m = m0 + 16 * b + r < M ? m0 + 16 * b + r : M - 1;
-    x[b] = X.codes + m * X.ld;
-    zx[b] = X.zero[m] + 128;
-    wide |= zx[b] != (int)(short)zx[b];
-  }
-  float acc[NT][MT][4];
+// The columns' slices: `n` (a power of two up to kSlices, a function of the columns
+// alone) of `per` runs each.  A slice is summed run by run; the sums of slices
+// 2 i and 2 i + 1 are added, then those of the pairs in order, whichever kernel
+// does it.
+constexpr int kSlices = 8;
+struct Slices {
+  int n, per;
+};
+
+template <int NT, int MT>
+__device__ __forceinline__ void zero_acc(float (&acc)[NT][MT][4]) {
 #pragma unroll
   for (int a = 0; a < NT; ++a)
 #pragma unroll
     for (int b = 0; b < MT; ++b)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[a][b][i] = 0.0f;
-  const int64_t runs = W.ld / 128, k0 = (int64_t)wave * per, k1 = k0 + per < runs ? k0 + per : runs;
-  if (__any(wide))
-    mul4_runs<G, MT, NT, true>(W, w, x, X.ld, zx, n0, q, k0, k1, acc);
+}
+// Four neighbouring results of row m: Y[m][n ..] = s qx / 16 + bias.
+template <class TY>
+__device__ __forceinline__ void put4(float4 s, int64_t m, int64_t n, int64_t rows, const ActRows &X,
+                                     const float *bias, TY *Y) {
+  const float qx = X.inv_q[m] * 0.0625f;
+  float y[4] = {s.x * qx, s.y * qx, s.z * qx, s.w * qx};
+  TY *o = Y + m * rows + n;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (bias && n + i < rows) y[i] += bias[n + i];
+  if (n + 4 <= rows) {
+    store_n<4>(o, y);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < rows) o[i] = (TY)y[i];
+  }
+}
+__device__ __forceinline__ float4 add4(float4 a, float4 b) {
+  return make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+}
+
+// Up to 16 rows of X: 16 rows of W a workgroup, a wave per slice.  What is read is W,
+// once, straight into registers, AHEAD runs at a time in flight.
+template <int G, bool WIDE, int AHEAD>
+__device__ __forceinline__ void mul4_slice(const Q4Mat &W, const uint8_t *w, const int8_t *x,
+                                           int64_t ldx, int zx0, int64_t n, int q, int64_t k0,
+                                           int64_t k1, float (&acc)[1][1][4]) {
+  const int zx[1] = {zx0};
+  for (int64_t k = k0; k < k1; k += AHEAD) {
+    uint4 wv[AHEAD][1];
+    int2 xv[AHEAD][1][4];
+    RunScales<G, 1> sc[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int64_t ku = k + u < k1 ? k + u : k1 - 1;
+      wv[u][0] = *reinterpret_cast<const uint4 *>(w + 64 * ku);
+      sc[u].load(W, ku, n);
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        // columns at and past ldx recover to 0 in W: any codes serve
+        const int64_t c = 128 * ku + 32 * p + 8 * q;
+        xv[u][0][p] = *reinterpret_cast<const int2 *>(x + (c < ldx ? c : 0));
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (k + u < k1) mul4_run<G, 1, 1, WIDE>(wv[u], xv[u], sc[u], zx, acc);
+  }
+}
+template <int G, class TY>
+__global__ __launch_bounds__(64 * kSlices) void k_matmul4_few(Q4Mat W, ActRows X, int64_t M,
+                                                              Slices sl,
+                                                              const float *__restrict__ bias,
+                                                              TY *__restrict__ Y) {
+  __shared__ float4 parts[kSlices][64];
+  constexpr int kAhead = G == 32 ? 2 : 4;
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
+  const int64_t n0 = (int64_t)blockIdx.x * 16, n = n0 + 4 * q;
+  const uint8_t *w =
+      W.codes + (n0 + r < W.rows ? n0 + r : W.rows - 1) * (W.ld / 2) + 16 * q;
+  const int64_t m = r < M ? r : M - 1;
+  const int8_t *x = X.codes + m * X.ld;
+  const int zx = X.zero[m] + 128;
+  float acc[1][1][4];
+  zero_acc(acc);
+  const int64_t runs = W.ld / 128, k0 = (int64_t)wave * sl.per,
+                k1 = k0 + sl.per < runs ? k0 + sl.per : runs;
+  if (__any(zx != (int)(short)zx))
+    mul4_slice<G, true, 1>(W, w, x, X.ld, zx, n, q, k0, k1, acc);
   else
-    mul4_runs<G, MT, NT, false>(W, w, x, X.ld, zx, n0, q, k0, k1, acc);
-  // the waves' sums, added in order
+    mul4_slice<G, false, kAhead>(W, w, x, X.ld, zx, n, q, k0, k1, acc);
+  parts[wave][lane] = make_float4(acc[0][0][0], acc[0][0][1], acc[0][0][2], acc[0][0][3]);
+  __syncthreads();
+  if (wave > 0 || n >= W.rows || r >= M) return;
+  float4 s = parts[0][lane];
+  if (sl.n > 1) s = add4(s, parts[1][lane]);
+  for (int p = 2; p < sl.n; p += 2) s = add4(s, add4(parts[p][lane], parts[p + 1][lane]));
+  put4(s, r, n, W.rows, X, bias, Y);
+}
+
+// More rows of X: a workgroup takes 32 NT rows of W and 16 MT of X.  Two waves share
+// the codes of a pair of slices, run by run through LDS, laid out there as the
+// lanes read them (their four 8-byte pieces together); W still goes straight to
+// registers.  The next run's loads are in flight while one is multiplied.
+template <int G, int MT, int NT, bool WIDE>
+__device__ __forceinline__ void mul4_pair(const Q4Mat &W, const ActRows &X, int64_t M,
+                                          const Slices &sl, int64_t m0, int64_t n0, int pair,
+                                          int half, const int (&zx)[MT], int8_t *lds,
+                                          float (&tot)[NT][MT][4]) {
+  constexpr int kPitch = 144;                 // bytes of a row's run in LDS: 128, and off the banks
+  constexpr int kBuf = 16 * MT * kPitch;
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+  const int64_t runs = W.ld / 128, k0 = (int64_t)pair * 2 * sl.per;
+  const int count = sl.n > 1 ? 2 * sl.per : sl.per;
+  const uint8_t *w[NT];
+#pragma unroll
+  for (int a = 0; a < NT; ++a) {
+    const int64_t n = n0 + 16 * a + r;
+    w[a] = W.codes + (n < W.rows ? n : W.rows - 1) * (W.ld / 2) + 16 * q;
+  }
+  // staging: 128 threads, a 16-byte chunk of every 16th row each
+  const int th = half * 64 + lane, chunk = th & 7;
+  const int8_t *src[MT];
+#pragma unroll
+  for (int b = 0; b < MT; ++b) {
+    const int64_t m = m0 + 16 * b + (th >> 3);
+    src[b] = X.codes + (m < M ? m : M - 1) * X.ld;
+  }
+  int4 xr[MT];
+  uint4 wn[NT];
+  RunScales<G, NT> sn;
+  auto fetch = [&](int64_t k) {
+    const int64_t c = 128 * k + 16 * chunk;
+#pragma unroll
+    for (int b = 0; b < MT; ++b)
+      xr[b] = *reinterpret_cast<const int4 *>(src[b] + (c < X.ld ? c : 0));
+#pragma unroll
+    for (int a = 0; a < NT; ++a) wn[a] = *reinterpret_cast<const uint4 *>(w[a] + 64 * k);
+    sn.load(W, k, n0 + 4 * q);
+  };
+  auto stage = [&](int buf) {  // columns 32 p + 8 i .. + 7 of a run to i 32 + p 8
+#pragma unroll
+    for (int b = 0; b < MT; ++b) {
+      int8_t *d = lds + buf * kBuf + (16 * b + (th >> 3)) * kPitch;
+      const int e = 2 * chunk;
+      *reinterpret_cast<int2 *>(d + (e & 3) * 32 + (e >> 2) * 8) = make_int2(xr[b].x, xr[b].y);
+      *reinterpret_cast<int2 *>(d + ((e + 1) & 3) * 32 + (e >> 2) * 8) =
+          make_int2(xr[b].z, xr[b].w);
+    }
+  };
+  float acc[NT][MT][4];
+  zero_acc(acc);
+  zero_acc(tot);
+  if (k0 < runs) {
+    fetch(k0);
+    stage(0);
+  }
+  __syncthreads();
+  for (int i = 0; i < count; ++i) {
+    const int64_t k = k0 + i;
+    uint4 wv[NT];
+    RunScales<G, NT> sc = sn;
+#pragma unroll
+    for (int a = 0; a < NT; ++a) wv[a] = wn[a];
+    const bool more = i + 1 < count && k + 1 < runs;
+    if (more) fetch(k + 1);
+    if (k < runs) {
+      int2 xv[MT][4];
+      const int8_t *d = lds + (i & 1) * kBuf + r * kPitch + 32 * q;
+#pragma unroll
+      for (int b = 0; b < MT; ++b)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int4 v = *reinterpret_cast<const int4 *>(d + 16 * b * kPitch + 16 * h);
+          xv[b][2 * h] = make_int2(v.x, v.y);
+          xv[b][2 * h + 1] = make_int2(v.z, v.w);
+        }
+      mul4_run<G, MT, NT, WIDE>(wv, xv, sc, zx, acc);
+    }
+    if (i + 1 == sl.per || i + 1 == count) {  // a slice ends
+#pragma unroll
+      for (int a = 0; a < NT; ++a)
+#pragma unroll
+        for (int b = 0; b < MT; ++b)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) tot[a][b][e] = i + 1 == sl.per ? acc[a][b][e] : tot[a][b][e] + acc[a][b][e];
+      zero_acc(acc);
+    }
+    if (more) stage((i + 1) & 1);
+    __syncthreads();
+  }
+}
+template <int G, int MT, int NT, class TY>
+__global__ __launch_bounds__(512) void k_matmul4(Q4Mat W, ActRows X, int64_t M, Slices sl,
+                                                 const float *__restrict__ bias,
+                                                 TY *__restrict__ Y) {
+  constexpr int kBuf = 16 * MT * 144;
+  // per pair two buffers of codes; after the loop the pairs' sums
+  extern __shared__ __attribute__((aligned(16))) int8_t lds[];
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
+  const int half = wave & 1, pair = wave >> 1, pairs = blockDim.x >> 7;
+  const int64_t n0 = (int64_t)blockIdx.x * 32 * NT + 16 * NT * half;
+  const int64_t m0 = (int64_t)blockIdx.y * 16 * MT;
+  int zx[MT];
+  bool wide = false;
+#pragma unroll
+  for (int b = 0; b < MT; ++b) {
+    const int64_t m = m0 + 16 * b + r < M ? m0 + 16 * b + r : M - 1;
+    zx[b] = X.zero[m] + 128;
+    wide |= zx[b] != (int)(short)zx[b];
+  }
+  // rows of W past the last: the last ones' loads, no stores (their scales' places
+  // are W.ldr wide, which 16 NT rows from n0 may pass)
+  const int64_t nl = n0 + 16 * NT <= W.ldr ? n0 : W.ldr - 16 * NT;
+  float tot[NT][MT][4];
+  if (__any(wide))  // (alike in every wave: all see the same rows of X)
+    mul4_pair<G, MT, NT, true>(W, X, M, sl, m0, nl, pair, half, zx, lds + pair * 2 * kBuf, tot);
+  else
+    mul4_pair<G, MT, NT, false>(W, X, M, sl, m0, nl, pair, half, zx, lds + pair * 2 * kBuf, tot);
+  float4 *parts = reinterpret_cast<float4 *>(lds);  // [pairs][2][NT MT][64]
 #pragma unroll
   for (int a = 0; a < NT; ++a)
 #pragma unroll
     for (int b = 0; b < MT; ++b)
-      parts[(wave * NT * MT + a * MT + b) * 64 + lane] =
-          make_float4(acc[a][b][0], acc[a][b][1], acc[a][b][2], acc[a][b][3]);
+      parts[((pair * 2 + half) * NT * MT + a * MT + b) * 64 + lane] =
+          make_float4(tot[a][b][0], tot[a][b][1], tot[a][b][2], tot[a][b][3]);
   __syncthreads();
-  for (int tile = wave; tile < NT * MT; tile += waves) {
-    const int64_t n = n0 + 16 * (tile / MT) + 4 * q, m = m0 + 16 * (tile % MT) + r;
-    if (n >= W.rows || m >= M) continue;
-    float4 s = parts[tile * 64 + lane];
-    for (int p = 1; p < waves; ++p) {
-      const float4 v = parts[(p * NT * MT + tile) * 64 + lane];
-      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-    }
-    const float qx = X.inv_q[m] * 0.0625f;
-    float y[4] = {s.x * qx, s.y * qx, s.z * qx, s.w * qx};
-    TY *o = Y + m * W.rows + n;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (bias && n + i < W.rows) y[i] += bias[n + i];
-    if (n + 4 <= W.rows) {
-      store_n<4>(o, y);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (n + i < W.rows) o[i] = (TY)y[i];
-    }
+  for (int tile = pair; tile < NT * MT; tile += pairs) {
+    const int64_t n = nl + 16 * (tile / MT) + 4 * q, m = m0 + 16 * (tile % MT) + r;
+    if (n < n0 || n >= W.rows || m >= M) continue;
+    float4 s = parts[(half * NT * MT + tile) * 64 + lane];
+    for (int p = 1; p < pairs; ++p)
+      s = add4(s, parts[((p * 2 + half) * NT * MT + tile) * 64 + lane]);
+    put4(s, m, n, W.rows, X, bias, Y);
   }
 }
 
@@ -383,39 +534,50 @@ hipError_t launch_quantize_rows_of(int type, const void *X, int64_t ldx, int64_t
 }
 
 template <int MT, int NT, class TY>
-static void run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, TY *Y,
-                        hipStream_t s) {
-  const int runs = (int)(W.ld / 128);
-  int waves = 1;
-  while (waves < kSlices && 2 * waves <= runs) waves *= 2;
-  const int per = (runs + waves - 1) / waves;
-  const dim3 grid(blocks_for(W.rows, 16 * NT), blocks_for(M, 16 * MT));
+static hipError_t run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const Slices &sl,
+                        const float *bias, TY *Y, hipStream_t s) {
+  const int pairs = sl.n > 1 ? sl.n / 2 : 1;
+  const size_t codes = (size_t)pairs * 2 * 16 * MT * 144;
+  const size_t sums = (size_t)pairs * 2 * NT * MT * 64 * sizeof(float4);
   auto kern = W.group == 32 ? k_matmul4<32, MT, NT, TY>
               : W.group == 64 ? k_matmul4<64, MT, NT, TY>
                               : k_matmul4<128, MT, NT, TY>;
-  hipLaunchKernelGGL(kern, grid, dim3(64 * waves), waves * NT * MT * 64 * sizeof(float4), s, W, X, M,
-                     per, bias, Y);
+  const size_t lds = std::max(codes, sums);
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(kern, dim3(blocks_for(W.rows, 32 * NT), blocks_for(M, 16 * MT)),
+                     dim3(128 * pairs), lds, s, W, X, M, sl, bias, Y);
+  return hipGetLastError();
 }
 template <class TY>
-static void run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, TY *Y,
-                        hipStream_t s) {
-  if (M <= 16)
-    run_matmul4<1, 1, TY>(W, X, M, bias, Y, s);
-  else if (M <= 32)
-    run_matmul4<2, 2, TY>(W, X, M, bias, Y, s);
-  else
-    run_matmul4<4, 2, TY>(W, X, M, bias, Y, s);
+static hipError_t run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, TY *Y,
+                              hipStream_t s) {
+  const int runs = (int)(W.ld / 128);
+  Slices sl{1, 0};
+  while (sl.n < kSlices && 2 * sl.n <= runs) sl.n *= 2;
+  sl.per = (runs + sl.n - 1) / sl.n;
+  if (M <= 16) {
+    auto kern = W.group == 32 ? k_matmul4_few<32, TY>
+                : W.group == 64 ? k_matmul4_few<64, TY>
+                                : k_matmul4_few<128, TY>;
+    hipLaunchKernelGGL(kern, dim3(blocks_for(W.rows, 16)), dim3(64 * sl.n), 0, s, W, X, M, sl, bias,
+                       Y);
+    return hipGetLastError();
+  }
+  if (M <= 32) return run_matmul4<2, 1, TY>(W, X, M, sl, bias, Y, s);
+  if (W.ldr >= 32 && W.rows * ((M + 63) / 64) >= 64 * 256)
+    return run_matmul4<4, 2, TY>(W, X, M, sl, bias, Y, s);
+  return run_matmul4<4, 1, TY>(W, X, M, sl, bias, Y, s);
 }
 hipError_t launch_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, int ytype,
                           void *Y, hipStream_t s) {
   if (M == 0 || W.rows == 0) return hipSuccess;
-  if (ytype == 0)
-    run_matmul4(W, X, M, bias, static_cast<float *>(Y), s);
-  else if (ytype == 1)
-    run_matmul4(W, X, M, bias, static_cast<f16 *>(Y), s);
-  else
-    run_matmul4(W, X, M, bias, static_cast<bf16 *>(Y), s);
-  return hipGetLastError();
+  if (ytype == 0) return run_matmul4(W, X, M, bias, static_cast<float *>(Y), s);
+  if (ytype == 1) return run_matmul4(W, X, M, bias, static_cast<f16 *>(Y), s);
+  return run_matmul4(W, X, M, bias, static_cast<bf16 *>(Y), s);
 }
 
 }  // namespace ql

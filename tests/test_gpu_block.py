@@ -360,6 +360,21 @@ def test_matmul4_slices_rows_that_are_not_finite_and_empty(ql):
     assert ql.matmul4(q, torch.empty(0, 200, device=DEV)).shape == (0, 90)
 
 
+@pytest.mark.parametrize("rows,cols", [(100, 60), (70, 300), (257, 1200), (300, 4097), (16500, 520)])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_matmul4_rows_do_not_depend_on_the_batch(ql, rows, cols, group):
+    """A row's result has the same bits alone and in any batch, zero points far off among
+    the others or not."""
+    z = gen(rows + cols)
+    q = ql.quantize4((0.05 * z(rows, cols)).to(DEV), group)
+    X = z(150, cols)
+    X[70:, :] = 9 + 0.0001 * X[70:, :]   # zero points past 16 bits
+    X = X.to(DEV)
+    alone = torch.cat([ql.matmul4(q, X[k:k + 1]) for k in range(150)])
+    for m in (2, 16, 17, 32, 33, 64, 65, 71, 150):
+        assert torch.equal(ql.matmul4(q, X[:m]), alone[:m]), m
+
+
 def test_matmul4_on_its_input(ql):
     """Y on X, as the 8-bit product allows."""
     z = gen(6)
