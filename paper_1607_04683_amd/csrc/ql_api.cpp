@@ -1572,10 +1572,13 @@ bool state_clash(const float *in, const float *out, size_t bytes) {
   return in != out && share_bytes(in, bytes, out, bytes);
 }
 
+// 64 rows of codes stay within 32-bit offsets.
+constexpr int64_t kMaxCols4 = (int64_t)1 << 25;
 ql_status check_qmatrix4(const ql_qmatrix4 *q) {
   if (!q || !q->codes || !q->zero || !q->inv_q) return QL_EINVAL;
   if (q->rows < 0 || q->cols <= 0 || q->rows > kMaxDim || q->cols > kMaxDim - 127) return QL_ESHAPE;
   if (q->group != 32 && q->group != 64 && q->group != 128) return QL_EUNSUPPORTED;
+  if (q->cols > kMaxCols4) return QL_EUNSUPPORTED;
   if (q->ld != round_up(q->cols, 128)) return QL_ESHAPE;
   if (!aligned(q->codes, 16) || !aligned(q->inv_q, 16) || !aligned(q->zero, 4)) return QL_EINVAL;
   return QL_OK;
@@ -1713,7 +1716,7 @@ ql_status ql_matmul4(const ql_qmatrix4 *W, const ql_qact *X, const float *bias, 
   const int64_t m = X->rows;
   if (m < 0 || X->cols != W->cols || X->ld % 64 != 0 || !rows_ok(X->ld, m, X->cols))
     return QL_ESHAPE;
-  if (!matmul4_rows_ok(m)) return QL_EUNSUPPORTED;
+  if (!matmul4_rows_ok(m) || X->ld > kMaxCols4) return QL_EUNSUPPORTED;
   if (m == 0 || W->rows == 0) return QL_OK;
   if (!X->codes || !X->zero || !X->inv_q || !Y || !aligned(X->codes, 16)) return QL_EINVAL;
   if (share_bytes(X->codes, (size_t)(m * X->ld), Y, (size_t)(m * W->rows) * type_size(t)))

@@ -268,4 +268,12 @@ static bool by_row(int64_t cols, F f) {
 }
 constexpr int block_of(int waves) { return waves == 1 ? 256 : 64 * waves; }
 
+// Barrier of a workgroup that orders LDS accesses alone: loads from memory stay in
+// flight over it (__syncthreads waits for them).
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 }  // namespace ql

@@ -145,110 +145,189 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void k_quantize_rows
   code_row<VEC, PER, WAVES, TAIL>(v, n, t, codes + row * ld, ld, zero + row, inv_q + row, sums + row);
 }
 
-// The product.  A wave takes 16 NT rows of W (lane: row r = lane & 15 of 16, share
-// q = lane >> 4 of the columns) and 16 MT rows of X.  Per group three products
-// on the matrix units: W X (16 sum c x), W 1 (16 sum c) and 1 X (sum x), with
-// c = V' - 8 and x = x' - 128; then, with z = z_g + 8 and zt = zx + 128,
-//   16 T_g = W X + [16 z, W 1 + 16 z G] . [1 X, zt]
+// The product.  A wave multiplies 16 MT rows of X (operand A) by 16 NT rows of W
+// (operand B; lane: row r = lane & 15 of 16, share q = lane >> 4 of the columns);
+// a lane's results are rows 4 q + i of X at row r of W.  Per group three products
+// on the matrix units: X W (16 sum x c), 1 W (16 sum c) and X 1 (sum x), with c =
+// V' - 8 and x = x' - 128; then, with z = z_g + 8 and zt = zx + 128,
+//   16 T_g = X W + [16 z, 1 W + 16 z G] . [X 1, zt]
 // is one 16-bit dot product onto the first's result, exact; one conversion and one
 // fma per group follow.  (Rows whose range lies so far off 0 that zt does not
 // fit 16 bits: the same in fp32, every term an integer below 2^24 but the last.)
+// With W as operand B a lane has one zero point and one scale per group, not four.
 //
 // The columns are cut into slices that the waves of a workgroup share, and the
 // slices' sums added in an order that depends on the matrix alone: a row's result
 // does not depend on the rows beside it.
-// One run's scales and zero points of the lane's 4 NT output rows.
+
+// One run's scales and zero points of the lane's NT rows of W.
 template <int G, int NT>
 struct RunScales {
   static constexpr int kParts = 128 / G;  // groups in a run
-  float4 q[kParts][NT];
+  float q[kParts][NT];
   int z[kParts][NT];
-  __device__ __forceinline__ void load(const Q4Mat &W, int64_t k, int64_t n) {
+  // (n0 and k are the wave's, r the lane's: addresses are scalars plus a lane's offset)
+  __device__ __forceinline__ void load(const Q4Mat &W, int k, int64_t n0, uint32_t r) {
+    const int64_t at = (int64_t)k * kParts * W.ldr + n0;
+    const float *qp = W.inv_q + at;
+    const int8_t *zp = W.zero + at;
 #pragma unroll
-    for (int gp = 0; gp < kParts; ++gp)
+    for (int gp = 0; gp < kParts; ++gp, qp += W.ldr, zp += W.ldr)
 #pragma unroll
       for (int a = 0; a < NT; ++a) {
-        const int64_t at = (k * kParts + gp) * W.ldr + n + 16 * a;
-        q[gp][a] = *reinterpret_cast<const float4 *>(W.inv_q + at);
-        z[gp][a] = *reinterpret_cast<const int *>(W.zero + at);
+        q[gp][a] = (qp + 16 * a)[r];
+        z[gp][a] = (zp + 16 * a)[r];
       }
   }
 };
 // One run: the lane's 16 bytes of each 16 rows of W against its codes of X, four
-// 8-byte pieces (32 columns apart) of each 16 rows.
-template <int G, int MT, int NT, bool WIDE>
+// 8-byte pieces (32 columns apart) of each 16 rows.  ROWS: how many of the lane's
+// four rows of X count.
+template <int G, int MT, int NT, int ROWS, bool WIDE>
 __device__ __forceinline__ void mul4_run(const uint4 (&wv)[NT], const int2 (&xv)[MT][4],
-                                         const RunScales<G, NT> &sc, const int (&zx)[MT],
-                                         float (&acc)[NT][MT][4]) {
+                                         const RunScales<G, NT> &sc, const int (&zx)[MT][ROWS],
+                                         float (&acc)[NT][MT][ROWS]) {
   constexpr int kParts = 128 / G;
   constexpr int kWords = 4 / kParts;  // words of a lane in a group
   const v4i one{0x01010101, 0x01010101, 0x01010101, 0x01010101};
+  const long one8 = 0x0101010101010101l;
   typedef short v2s __attribute__((ext_vector_type(2)));
+  auto pair = [](uint32_t lo, uint32_t hi) { return (long)(((uint64_t)hi << 32) | lo); };
+  auto quad = [&](int b, int p) {
+    return v4i{xv[b][p].x, xv[b][p].y, xv[b][p + 1].x, xv[b][p + 1].y};
+  };
 #pragma unroll
   for (int gp = 0; gp < kParts; ++gp) {
     v4i x1[MT];
 #pragma unroll
-    for (int b = 0; b < MT; ++b) x1[b] = v4i{};
-    auto pair = [](uint32_t lo, uint32_t hi) { return (long)(((uint64_t)hi << 32) | lo); };
-    const long one8 = 0x0101010101010101l;
-#pragma unroll
     for (int b = 0; b < MT; ++b) {
+      x1[b] = v4i{};
       if constexpr (kWords >= 2) {
 #pragma unroll
         for (int p = gp * kWords; p < (gp + 1) * kWords; p += 2)
-          x1[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
-              one, v4i{xv[b][p].x, xv[b][p].y, xv[b][p + 1].x, xv[b][p + 1].y}, x1[b], 0, 0, 0);
+          x1[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(quad(b, p), one, x1[b], 0, 0, 0);
       } else {
         x1[b] = __builtin_amdgcn_mfma_i32_16x16x32_i8(
-            one8, pair((uint32_t)xv[b][gp].x, (uint32_t)xv[b][gp].y), x1[b], 0, 0, 0);
+            pair((uint32_t)xv[b][gp].x, (uint32_t)xv[b][gp].y), one8, x1[b], 0, 0, 0);
       }
     }
 #pragma unroll
     for (int a = 0; a < NT; ++a) {
       const uint32_t ww[4] = {wv[a].x, wv[a].y, wv[a].z, wv[a].w};
-      v4i wx[MT], w1{};
+      v4i xw[MT], w1{};
 #pragma unroll
-      for (int b = 0; b < MT; ++b) wx[b] = v4i{};
+      for (int b = 0; b < MT; ++b) xw[b] = v4i{};
       if constexpr (kWords >= 2) {
 #pragma unroll
         for (int p = gp * kWords; p < (gp + 1) * kWords; p += 2) {
-          const v4i wa{(int)((ww[p] << 4) & kHigh), (int)(ww[p] & kHigh),
+          const v4i wb{(int)((ww[p] << 4) & kHigh), (int)(ww[p] & kHigh),
                        (int)((ww[p + 1] << 4) & kHigh), (int)(ww[p + 1] & kHigh)};
-          w1 = __builtin_amdgcn_mfma_i32_16x16x64_i8(wa, one, w1, 0, 0, 0);
+          w1 = __builtin_amdgcn_mfma_i32_16x16x64_i8(one, wb, w1, 0, 0, 0);
 #pragma unroll
           for (int b = 0; b < MT; ++b)
-            wx[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
-                wa, v4i{xv[b][p].x, xv[b][p].y, xv[b][p + 1].x, xv[b][p + 1].y}, wx[b], 0, 0, 0);
+            xw[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(quad(b, p), wb, xw[b], 0, 0, 0);
         }
       } else {
-        const long wa = pair((ww[gp] << 4) & kHigh, ww[gp] & kHigh);
-        w1 = __builtin_amdgcn_mfma_i32_16x16x32_i8(wa, one8, w1, 0, 0, 0);
+        const long wb = pair((ww[gp] << 4) & kHigh, ww[gp] & kHigh);
+        w1 = __builtin_amdgcn_mfma_i32_16x16x32_i8(one8, wb, w1, 0, 0, 0);
 #pragma unroll
         for (int b = 0; b < MT; ++b)
-          wx[b] = __builtin_amdgcn_mfma_i32_16x16x32_i8(
-              wa, pair((uint32_t)xv[b][gp].x, (uint32_t)xv[b][gp].y), wx[b], 0, 0, 0);
+          xw[b] = __builtin_amdgcn_mfma_i32_16x16x32_i8(
+              pair((uint32_t)xv[b][gp].x, (uint32_t)xv[b][gp].y), wb, xw[b], 0, 0, 0);
       }
-      const float qs[4] = {sc.q[gp][a].x, sc.q[gp][a].y, sc.q[gp][a].z, sc.q[gp][a].w};
+      const int z16 = 16 * sc.z[gp][a] + 128;
+      const int ws = w1[0] + z16 * G;  // (every row of 1 W is alike)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int z16 = 16 * ((int)(int8_t)(sc.z[gp][a] >> (8 * i)) + 8);
-        const int ws = w1[i] + z16 * G;
+      for (int b = 0; b < MT; ++b)
 #pragma unroll
-        for (int b = 0; b < MT; ++b) {
-          // (every row of 1 X is alike)
+        for (int i = 0; i < ROWS; ++i) {
           float t;
           if constexpr (WIDE) {
-            t = __builtin_fmaf((float)z16, (float)x1[b][0], (float)wx[b][i]);
-            t = __builtin_fmaf((float)zx[b], (float)ws, t);
+            t = __builtin_fmaf((float)z16, (float)x1[b][i], (float)xw[b][i]);
+            t = __builtin_fmaf((float)zx[b][i], (float)ws, t);
           } else {
-            const v2s u{(short)z16, (short)ws}, v{(short)x1[b][0], (short)zx[b]};
-            t = (float)__builtin_amdgcn_sdot2(u, v, wx[b][i], false);
+            const v2s u{(short)z16, (short)ws}, v{(short)x1[b][i], (short)zx[b][i]};
+            t = (float)__builtin_amdgcn_sdot2(u, v, xw[b][i], false);
           }
-          acc[a][b][i] = __builtin_fmaf(qs[i], t, acc[a][b][i]);
+          acc[a][b][i] = __builtin_fmaf(sc.q[gp][a], t, acc[a][b][i]);
         }
+    }
+  }
+}
+// The same with the codes of X in LDS (the lane's four pieces of a row together, at d
+// + 16 b PITCH), read group by group, and the rows' zero points + 128 as pairs of
+// 16 bits in zs; where one is WIDE, whole from LDS (zl, the lane's first row's).
+template <int G, int MT, bool WIDE>
+__device__ __forceinline__ void mul4_run_lds(const uint4 &wv, const int8_t *d, int pitch,
+                                             const RunScales<G, 1> &sc, const int (&zs)[MT][2],
+                                             const int *zl, float (&acc)[MT][4]) {
+  constexpr int kParts = 128 / G;
+  constexpr int kWords = 4 / kParts;  // words of a lane in a group
+  const v4i one{0x01010101, 0x01010101, 0x01010101, 0x01010101};
+  const long one8 = 0x0101010101010101l;
+  typedef short v2s __attribute__((ext_vector_type(2)));
+  auto pair = [](uint32_t lo, uint32_t hi) { return (long)(((uint64_t)hi << 32) | lo); };
+  const uint32_t ww[4] = {wv.x, wv.y, wv.z, wv.w};
+#pragma unroll
+  for (int gp = 0; gp < kParts; ++gp) {
+    v4i wb[(kWords + 1) / 2], w1{};
+#pragma unroll
+    for (int h = 0; h < (kWords + 1) / 2; ++h) {
+      const uint32_t a = ww[gp * kWords + 2 * h], b = kWords >= 2 ? ww[(gp * kWords + 2 * h + 1) & 3] : 0;
+      wb[h] = v4i{(int)((a << 4) & kHigh), (int)(a & kHigh), (int)((b << 4) & kHigh), (int)(b & kHigh)};
+      if constexpr (kWords >= 2)
+        w1 = __builtin_amdgcn_mfma_i32_16x16x64_i8(one, wb[h], w1, 0, 0, 0);
+      else
+        w1 = __builtin_amdgcn_mfma_i32_16x16x32_i8(one8, pair(wb[h][0], wb[h][1]), w1, 0, 0, 0);
+    }
+    const int z16 = 16 * sc.z[gp][0] + 128;
+    const int ws = w1[0] + z16 * G;  // (every row of 1 W is alike)
+#pragma unroll
+    for (int b = 0; b < MT; ++b) {
+      v4i x1{}, xw{};
+      if constexpr (kWords >= 2) {
+#pragma unroll
+        for (int h = 0; h < kWords / 2; ++h) {
+          const v4i x = *reinterpret_cast<const v4i *>(d + 16 * b * pitch + 8 * (gp * kWords + 2 * h));
+          x1 = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, one, x1, 0, 0, 0);
+          xw = __builtin_amdgcn_mfma_i32_16x16x64_i8(x, wb[h], xw, 0, 0, 0);
+        }
+      } else {
+        const long x = *reinterpret_cast<const long *>(d + 16 * b * pitch + 8 * gp);
+        x1 = __builtin_amdgcn_mfma_i32_16x16x32_i8(x, one8, x1, 0, 0, 0);
+        xw = __builtin_amdgcn_mfma_i32_16x16x32_i8(x, pair(wb[0][0], wb[0][1]), xw, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float t;
+        if constexpr (WIDE) {
+          t = __builtin_fmaf((float)z16, (float)x1[i], (float)xw[i]);
+          t = __builtin_fmaf((float)zl[16 * b + i], (float)ws, t);
+        } else {
+          const v2s u{(short)z16, (short)ws};
+          const v2s v{(short)x1[i], (short)(zs[b][i / 2] >> (16 * (i & 1)))};
+          t = (float)__builtin_amdgcn_sdot2(u, v, xw[i], false);
+        }
+        acc[b][i] = __builtin_fmaf(sc.q[gp][0], t, acc[b][i]);
       }
     }
   }
+}
+// Zero points (+ 128) of rows m0 + 16 b + 4 q + i of X, in range; whether one of the
+// wave's does not fit 16 bits (alike in every wave that has the same rows).
+template <int MT, int ROWS>
+__device__ __forceinline__ bool load_zeros(const ActRows &X, int64_t M, int64_t m0, int q,
+                                           int (&zx)[MT][ROWS]) {
+  bool wide = false;
+#pragma unroll
+  for (int b = 0; b < MT; ++b)
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const int64_t m = m0 + 16 * b + 4 * q + i;
+      zx[b][i] = X.zero[m < M ? m : M - 1] + 128;
+      wide |= zx[b][i] != (int)(short)zx[b][i];
+    }
+  return wide;
 }
 
 // The columns' slices: `n` (a power of two up to kSlices, a function of the columns
@@ -260,20 +339,34 @@ struct Slices {
   int n, per;
 };
 
-template <int NT, int MT>
-__device__ __forceinline__ void zero_acc(float (&acc)[NT][MT][4]) {
+// Workgroup b of a launch goes to XCD b % 8, each with its own L2: those of one XCD
+// take neighbouring rows of W, whose scales and zero points share cache lines, and
+// all rows of X for them.  Tiles beyond the last: none.
+struct Tile {
+  int64_t n, m;
+};
+__device__ __forceinline__ Tile tile_of(int64_t b, int64_t ntiles, int64_t mtiles) {
+  const int64_t j = b >> 3, per = (ntiles + 7) >> 3, jn = j / mtiles;
+  return Tile{(b & 7) * per + jn, j - jn * mtiles};
+}
+inline unsigned tile_grid(int64_t ntiles, int64_t mtiles) {
+  return (unsigned)(8 * ((ntiles + 7) / 8) * mtiles);
+}
+
+template <int NT, int MT, int ROWS>
+__device__ __forceinline__ void zero_acc(float (&acc)[NT][MT][ROWS]) {
 #pragma unroll
   for (int a = 0; a < NT; ++a)
 #pragma unroll
     for (int b = 0; b < MT; ++b)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[a][b][i] = 0.0f;
+      for (int i = 0; i < ROWS; ++i) acc[a][b][i] = 0.0f;
 }
 // Four neighbouring results of row m: Y[m][n ..] = s qx / 16 + bias.
 template <class TY>
-__device__ __forceinline__ void put4(float4 s, int64_t m, int64_t n, int64_t rows, const ActRows &X,
+__device__ __forceinline__ void put4(float4 s, int64_t m, int64_t n, int64_t rows, float inv_q,
                                      const float *bias, TY *Y) {
-  const float qx = X.inv_q[m] * 0.0625f;
+  const float qx = inv_q * 0.0625f;
   float y[4] = {s.x * qx, s.y * qx, s.z * qx, s.w * qx};
   TY *o = Y + m * rows + n;
 #pragma unroll
@@ -292,198 +385,205 @@ __device__ __forceinline__ float4 add4(float4 a, float4 b) {
 }
 
 // Up to 16 rows of X: 16 rows of W a workgroup, a wave per slice.  What is read is W,
-// once, straight into registers, AHEAD runs at a time in flight.
-template <int G, bool WIDE, int AHEAD>
-__device__ __forceinline__ void mul4_slice(const Q4Mat &W, const uint8_t *w, const int8_t *x,
-                                           int64_t ldx, int zx0, int64_t n, int q, int64_t k0,
-                                           int64_t k1, float (&acc)[1][1][4]) {
-  const int zx[1] = {zx0};
-  for (int64_t k = k0; k < k1; k += AHEAD) {
+// once, straight into registers, AHEAD runs at a time in flight.  ROWS: 1, 2 or 4
+// by the rows of X (up to four lie in the lanes with q = 0).
+template <int G, int ROWS, int AHEAD, class TY>
+__global__ __launch_bounds__(64 * kSlices) void k_matmul4_few(Q4Mat W, ActRows X, int64_t M,
+                                                              Slices sl,
+                                                              const float *__restrict__ bias,
+                                                              TY *__restrict__ Y) {
+  __shared__ __attribute__((aligned(16))) float parts[kSlices][16][16];
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n0 = tile_of(blockIdx.x, W.ldr / 16, 1).n * 16;
+  if (n0 >= W.rows) return;
+  int zx[1][ROWS];
+  bool wide = load_zeros<1, ROWS>(X, M, 0, q, zx);
+  const uint8_t *w = W.codes + n0 * (W.ld / 2);
+  const uint32_t wo = (uint32_t)((n0 + r < W.rows ? r : W.rows - 1 - n0) * (W.ld / 2)) + 16 * q;
+  const uint32_t xo = (uint32_t)((r < M ? r : M - 1) * X.ld) + 8 * q;
+  // this lane's part of the joining: row lane / 4 of X at rows n0 + 4 (lane & 3) .. of W
+  const int jm = lane >> 2;
+  const float jq = X.inv_q[jm < M ? jm : M - 1];
+  float acc[1][1][ROWS];
+  zero_acc(acc);
+  const int runs = (int)(W.ld / 128), k0 = wave * sl.per,
+            k1 = k0 + sl.per < runs ? k0 + sl.per : runs;
+  for (int k = k0; k < k1; k += AHEAD) {
     uint4 wv[AHEAD][1];
     int2 xv[AHEAD][1][4];
     RunScales<G, 1> sc[AHEAD];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      const int64_t ku = k + u < k1 ? k + u : k1 - 1;
-      wv[u][0] = *reinterpret_cast<const uint4 *>(w + 64 * ku);
-      sc[u].load(W, ku, n);
+      const int ku = k + u < k1 ? k + u : k1 - 1;
+      wv[u][0] = *reinterpret_cast<const uint4 *>((w + 64 * (int64_t)ku) + wo);
+      // X.ld is a multiple of 64: past it (columns that recover to 0 in W) any codes serve
+      const int8_t *x = X.codes + 128 * (int64_t)ku;
+      const int high = 128 * (int64_t)ku + 64 < X.ld ? 64 : 0;
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        // columns at and past ldx recover to 0 in W: any codes serve
-        const int64_t c = 128 * ku + 32 * p + 8 * q;
-        xv[u][0][p] = *reinterpret_cast<const int2 *>(x + (c < ldx ? c : 0));
-      }
+      for (int p = 0; p < 4; ++p)
+        xv[u][0][p] = *reinterpret_cast<const int2 *>((x + (p >= 2 ? high : 0) + 32 * (p & 1)) + xo);
+      sc[u].load(W, ku, n0, r);
     }
+    if (k == k0) wide = __any(wide);
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-      if (k + u < k1) mul4_run<G, 1, 1, WIDE>(wv[u], xv[u], sc[u], zx, acc);
+    for (int u = 0; u < AHEAD; ++u) {
+      if (k + u >= k1) break;
+      if (wide)
+        mul4_run<G, 1, 1, ROWS, true>(wv[u], xv[u], sc[u], zx, acc);
+      else
+        mul4_run<G, 1, 1, ROWS, false>(wv[u], xv[u], sc[u], zx, acc);
+    }
   }
-}
-template <int G, class TY>
-__global__ __launch_bounds__(64 * kSlices) void k_matmul4_few(Q4Mat W, ActRows X, int64_t M,
-                                                              Slices sl,
-                                                              const float *__restrict__ bias,
-                                                              TY *__restrict__ Y) {
-  __shared__ float4 parts[kSlices][64];
-  constexpr int kAhead = G == 32 ? 2 : 4;
-  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
-  const int64_t n0 = (int64_t)blockIdx.x * 16, n = n0 + 4 * q;
-  const uint8_t *w =
-      W.codes + (n0 + r < W.rows ? n0 + r : W.rows - 1) * (W.ld / 2) + 16 * q;
-  const int64_t m = r < M ? r : M - 1;
-  const int8_t *x = X.codes + m * X.ld;
-  const int zx = X.zero[m] + 128;
-  float acc[1][1][4];
-  zero_acc(acc);
-  const int64_t runs = W.ld / 128, k0 = (int64_t)wave * sl.per,
-                k1 = k0 + sl.per < runs ? k0 + sl.per : runs;
-  if (__any(zx != (int)(short)zx))
-    mul4_slice<G, true, 1>(W, w, x, X.ld, zx, n, q, k0, k1, acc);
-  else
-    mul4_slice<G, false, kAhead>(W, w, x, X.ld, zx, n, q, k0, k1, acc);
-  parts[wave][lane] = make_float4(acc[0][0][0], acc[0][0][1], acc[0][0][2], acc[0][0][3]);
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) parts[wave][4 * q + i][r] = acc[0][0][i];
   __syncthreads();
-  if (wave > 0 || n >= W.rows || r >= M) return;
-  float4 s = parts[0][lane];
-  if (sl.n > 1) s = add4(s, parts[1][lane]);
-  for (int p = 2; p < sl.n; p += 2) s = add4(s, add4(parts[p][lane], parts[p + 1][lane]));
-  put4(s, r, n, W.rows, X, bias, Y);
+  const int64_t n = n0 + 4 * (lane & 3);
+  if (wave > 0 || n >= W.rows || jm >= M) return;
+  auto part = [&](int p) { return *reinterpret_cast<const float4 *>(&parts[p][jm][4 * (lane & 3)]); };
+  float4 s = part(0);
+  if (sl.n > 1) s = add4(s, part(1));
+  for (int p = 2; p < sl.n; p += 2) s = add4(s, add4(part(p), part(p + 1)));
+  put4(s, jm, n, W.rows, jq, bias, Y);
 }
 
-// More rows of X: a workgroup takes 32 NT rows of W and 16 MT of X.  Two waves share
-// the codes of a pair of slices, run by run through LDS, laid out there as the
-// lanes read them (their four 8-byte pieces together); W still goes straight to
-// registers.  The next run's loads are in flight while one is multiplied.
-template <int G, int MT, int NT, bool WIDE>
-__device__ __forceinline__ void mul4_pair(const Q4Mat &W, const ActRows &X, int64_t M,
-                                          const Slices &sl, int64_t m0, int64_t n0, int pair,
-                                          int half, const int (&zx)[MT], int8_t *lds,
-                                          float (&tot)[NT][MT][4]) {
-  constexpr int kPitch = 144;                 // bytes of a row's run in LDS: 128, and off the banks
-  constexpr int kBuf = 16 * MT * kPitch;
+// More rows of X: a workgroup takes 16 NS rows of W and 32 of X, its waves NS of rows
+// times the parts that the pairs of slices are shared by.  The NS waves of a part
+// share the codes of X, run by run through LDS, laid out there as the lanes read
+// them (their four 8-byte pieces together); W goes straight to registers, two
+// runs ahead.  Every pair's sums go to LDS as it ends.
+constexpr int kPitch = 144;  // bytes of a row's run in LDS: 128, and off the banks
+constexpr int kMT = 2;       // tiles of 16 rows of X
+template <int G, int NS, class TY>
+__global__ __launch_bounds__(512, 4) void k_matmul4(Q4Mat W, ActRows X, int64_t M, Slices sl,
+                                                    const float *__restrict__ bias,
+                                                    TY *__restrict__ Y) {
+  constexpr int kBuf = 16 * kMT * kPitch, kAhead = 2, kChunks = 2 * kMT / NS;
+  extern __shared__ __attribute__((aligned(16))) int8_t shared[];  // [parts][2][kBuf], sums
+  __shared__ __attribute__((aligned(16))) int zl[16 * kMT];
   const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
-  const int64_t runs = W.ld / 128, k0 = (int64_t)pair * 2 * sl.per;
-  const int count = sl.n > 1 ? 2 * sl.per : sl.per;
-  const uint8_t *w[NT];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int part = wave / NS, sub = wave % NS, parts = (blockDim.x >> 6) / NS;
+  const int pairs = sl.n > 1 ? sl.n / 2 : 1;
+  const Tile tile0 = tile_of(blockIdx.x, (W.rows + 16 * NS - 1) / (16 * NS),
+                             (M + 16 * kMT - 1) / (16 * kMT));
+  if (tile0.n * 16 * NS >= W.rows) return;
+  const int64_t own = (tile0.n * NS + sub) * 16, m0 = tile0.m * 16 * kMT;
+  // past the last rows of W: the last ones' loads, no stores
+  const int64_t n0 = own + 16 <= W.ldr ? own : W.ldr - 16;
+  int8_t *lds = shared + part * 2 * kBuf;
+  float *sums = reinterpret_cast<float *>(shared + parts * 2 * kBuf);  // [pairs][NS][kMT][16][16]
+  const int per_pair = sl.n > 1 ? 2 * sl.per : sl.per;
+  const int runs = (int)(W.ld / 128), k0 = part * (pairs / parts) * per_pair;
+  const int count = (pairs / parts) * per_pair;
+  const uint8_t *w = W.codes + n0 * (W.ld / 2);
+  const uint32_t wo = (uint32_t)((n0 + r < W.rows ? r : W.rows - 1 - n0) * (W.ld / 2)) + 16 * q;
+  // staging: 64 NS threads, a 16-byte chunk of every 8 NS-th row each
+  const int th = sub * 64 + lane, chunk = th & 7;
+  const int8_t *xt = X.codes + m0 * X.ld;
+  uint32_t xo[kChunks];
 #pragma unroll
-  for (int a = 0; a < NT; ++a) {
-    const int64_t n = n0 + 16 * a + r;
-    w[a] = W.codes + (n < W.rows ? n : W.rows - 1) * (W.ld / 2) + 16 * q;
+  for (int b = 0; b < kChunks; ++b) {
+    const int64_t m = 8 * NS * b + (th >> 3);
+    xo[b] = (uint32_t)((m0 + m < M ? m : M - 1 - m0) * X.ld);
   }
-  // staging: 128 threads, a 16-byte chunk of every 16th row each
-  const int th = half * 64 + lane, chunk = th & 7;
-  const int8_t *src[MT];
-#pragma unroll
-  for (int b = 0; b < MT; ++b) {
-    const int64_t m = m0 + 16 * b + (th >> 3);
-    src[b] = X.codes + (m < M ? m : M - 1) * X.ld;
-  }
-  int4 xr[MT];
-  uint4 wn[NT];
-  RunScales<G, NT> sn;
-  auto fetch = [&](int64_t k) {
-    const int64_t c = 128 * k + 16 * chunk;
-#pragma unroll
-    for (int b = 0; b < MT; ++b)
-      xr[b] = *reinterpret_cast<const int4 *>(src[b] + (c < X.ld ? c : 0));
-#pragma unroll
-    for (int a = 0; a < NT; ++a) wn[a] = *reinterpret_cast<const uint4 *>(w[a] + 64 * k);
-    sn.load(W, k, n0 + 4 * q);
+  // What is in flight: W and its scales kAhead runs ahead, the codes of X one.  Loaded
+  // without branches, the last run again past it: only so are the compiler's waits
+  // for these loads and no others.
+  int4 xr[kChunks];
+  uint4 wr[kAhead];
+  RunScales<G, 1> sr[kAhead];
+  const int last = count < runs - k0 ? count : runs - k0;  // runs of this part (or none)
+  auto run_of = [&](int i) { return k0 + i < runs ? k0 + i : runs - 1; };
+  auto fetch_w = [&](int i, int slot) {
+    const int k = run_of(i);
+    wr[slot] = *reinterpret_cast<const uint4 *>((w + 64 * (int64_t)k) + wo);
+    sr[slot].load(W, k, n0, r);
   };
-  auto stage = [&](int buf) {  // columns 32 p + 8 i .. + 7 of a run to i 32 + p 8
+  auto fetch_x = [&](int i) {
+    const int64_t c = 128 * (int64_t)run_of(i);
+    // X.ld is a multiple of 64: past it (columns that recover to 0 in W) any codes serve
+    const uint32_t co = 16 * (chunk & (c + 64 < X.ld ? 7 : 3));
 #pragma unroll
-    for (int b = 0; b < MT; ++b) {
-      int8_t *d = lds + buf * kBuf + (16 * b + (th >> 3)) * kPitch;
+    for (int b = 0; b < kChunks; ++b)
+      xr[b] = *reinterpret_cast<const int4 *>((xt + c) + (xo[b] + co));
+  };
+  auto stage = [&](int slot) {  // columns 32 p + 8 i .. + 7 of a run to i 32 + p 8
+#pragma unroll
+    for (int b = 0; b < kChunks; ++b) {
+      int8_t *d = lds + slot * kBuf + (8 * NS * b + (th >> 3)) * kPitch;
       const int e = 2 * chunk;
       *reinterpret_cast<int2 *>(d + (e & 3) * 32 + (e >> 2) * 8) = make_int2(xr[b].x, xr[b].y);
       *reinterpret_cast<int2 *>(d + ((e + 1) & 3) * 32 + (e >> 2) * 8) =
           make_int2(xr[b].z, xr[b].w);
     }
   };
-  float acc[NT][MT][4];
-  zero_acc(acc);
-  zero_acc(tot);
-  if (k0 < runs) {
-    fetch(k0);
-    stage(0);
+  int zx[kMT][4];
+  bool wide = load_zeros<kMT, 4>(X, M, m0, q, zx);
+  fetch_x(0);
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) fetch_w(u, u);
+  int zs[kMT][2];
+#pragma unroll
+  for (int b = 0; b < kMT; ++b) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) zs[b][i] = (zx[b][2 * i] & 0xffff) | zx[b][2 * i + 1] << 16;
+    if (wave == 0 && r == 0)
+      *reinterpret_cast<int4 *>(&zl[16 * b + 4 * q]) =
+          make_int4(zx[b][0], zx[b][1], zx[b][2], zx[b][3]);
   }
-  __syncthreads();
-  for (int i = 0; i < count; ++i) {
-    const int64_t k = k0 + i;
-    uint4 wv[NT];
-    RunScales<G, NT> sc = sn;
+  float acc[kMT][4], tot[kMT][4];
 #pragma unroll
-    for (int a = 0; a < NT; ++a) wv[a] = wn[a];
-    const bool more = i + 1 < count && k + 1 < runs;
-    if (more) fetch(k + 1);
-    if (k < runs) {
-      int2 xv[MT][4];
-      const int8_t *d = lds + (i & 1) * kBuf + r * kPitch + 32 * q;
+  for (int b = 0; b < kMT; ++b)
 #pragma unroll
-      for (int b = 0; b < MT; ++b)
+    for (int e = 0; e < 4; ++e) acc[b][e] = tot[b][e] = 0.0f;
+  stage(0);
+  lds_barrier();
+  auto product = [&](auto is_wide) {
+    int in_slice = 0, slice = part * (pairs / parts) * 2;
+    for (int i0 = 0; i0 < count; i0 += kAhead) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int4 v = *reinterpret_cast<const int4 *>(d + 16 * b * kPitch + 16 * h);
-          xv[b][2 * h] = make_int2(v.x, v.y);
-          xv[b][2 * h + 1] = make_int2(v.z, v.w);
+      for (int u = 0; u < kAhead; ++u) {
+        const int i = i0 + u;
+        fetch_x(i + 1);
+        if (i < last)
+          mul4_run_lds<G, kMT, decltype(is_wide)::value>(
+              wr[u], lds + (u & 1) * kBuf + r * kPitch + 32 * q, kPitch, sr[u], zs, zl + 4 * q, acc);
+        fetch_w(i + kAhead, u);
+        if (++in_slice == sl.per && i < count) {  // a slice ends
+          in_slice = 0;
+          if ((slice & 1) || sl.n == 1) {
+            float *o = sums + (((slice >> 1) * NS + sub) * kMT) * 256 + 64 * q + r;
+#pragma unroll
+            for (int b = 0; b < kMT; ++b)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                o[b * 256 + 16 * e] = sl.n == 1 ? acc[b][e] : tot[b][e] + acc[b][e];
+          }
+#pragma unroll
+          for (int b = 0; b < kMT; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tot[b][e] = acc[b][e], acc[b][e] = 0.0f;
+          ++slice;
         }
-      mul4_run<G, MT, NT, WIDE>(wv, xv, sc, zx, acc);
+        stage((u + 1) & 1);
+        lds_barrier();
+      }
     }
-    if (i + 1 == sl.per || i + 1 == count) {  // a slice ends
-#pragma unroll
-      for (int a = 0; a < NT; ++a)
-#pragma unroll
-        for (int b = 0; b < MT; ++b)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) tot[a][b][e] = i + 1 == sl.per ? acc[a][b][e] : tot[a][b][e] + acc[a][b][e];
-      zero_acc(acc);
-    }
-    if (more) stage((i + 1) & 1);
-    __syncthreads();
-  }
-}
-template <int G, int MT, int NT, class TY>
-__global__ __launch_bounds__(512) void k_matmul4(Q4Mat W, ActRows X, int64_t M, Slices sl,
-                                                 const float *__restrict__ bias,
-                                                 TY *__restrict__ Y) {
-  constexpr int kBuf = 16 * MT * 144;
-  // per pair two buffers of codes; after the loop the pairs' sums
-  extern __shared__ __attribute__((aligned(16))) int8_t lds[];
-  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
-  const int half = wave & 1, pair = wave >> 1, pairs = blockDim.x >> 7;
-  const int64_t n0 = (int64_t)blockIdx.x * 32 * NT + 16 * NT * half;
-  const int64_t m0 = (int64_t)blockIdx.y * 16 * MT;
-  int zx[MT];
-  bool wide = false;
-#pragma unroll
-  for (int b = 0; b < MT; ++b) {
-    const int64_t m = m0 + 16 * b + r < M ? m0 + 16 * b + r : M - 1;
-    zx[b] = X.zero[m] + 128;
-    wide |= zx[b] != (int)(short)zx[b];
-  }
-  // rows of W past the last: the last ones' loads, no stores (their scales' places
-  // are W.ldr wide, which 16 NT rows from n0 may pass)
-  const int64_t nl = n0 + 16 * NT <= W.ldr ? n0 : W.ldr - 16 * NT;
-  float tot[NT][MT][4];
-  if (__any(wide))  // (alike in every wave: all see the same rows of X)
-    mul4_pair<G, MT, NT, true>(W, X, M, sl, m0, nl, pair, half, zx, lds + pair * 2 * kBuf, tot);
+  };
+  if (__any(wide))  // (alike in every wave: all have the same rows of X)
+    product(std::true_type());
   else
-    mul4_pair<G, MT, NT, false>(W, X, M, sl, m0, nl, pair, half, zx, lds + pair * 2 * kBuf, tot);
-  float4 *parts = reinterpret_cast<float4 *>(lds);  // [pairs][2][NT MT][64]
-#pragma unroll
-  for (int a = 0; a < NT; ++a)
-#pragma unroll
-    for (int b = 0; b < MT; ++b)
-      parts[((pair * 2 + half) * NT * MT + a * MT + b) * 64 + lane] =
-          make_float4(tot[a][b][0], tot[a][b][1], tot[a][b][2], tot[a][b][3]);
-  __syncthreads();
-  for (int tile = pair; tile < NT * MT; tile += pairs) {
-    const int64_t n = nl + 16 * (tile / MT) + 4 * q, m = m0 + 16 * (tile % MT) + r;
-    if (n < n0 || n >= W.rows || m >= M) continue;
-    float4 s = parts[(half * NT * MT + tile) * 64 + lane];
-    for (int p = 1; p < pairs; ++p)
-      s = add4(s, parts[((p * 2 + half) * NT * MT + tile) * 64 + lane]);
-    put4(s, m, n, W.rows, X, bias, Y);
+    product(std::false_type());
+  for (int tile = part; tile < kMT; tile += parts) {
+    const int64_t n = n0 + 4 * (lane & 3), m = m0 + 16 * tile + (lane >> 2);
+    if (n < own || n >= W.rows || m >= M) continue;
+    auto sum = [&](int p) {
+      return *reinterpret_cast<const float4 *>(&sums[((p * NS + sub) * kMT + tile) * 256 + 4 * lane]);
+    };
+    float4 s = sum(0);
+    for (int p = 1; p < pairs; ++p) s = add4(s, sum(p));
+    put4(s, m, n, W.rows, X.inv_q[m], bias, Y);
   }
 }
 
@@ -533,23 +633,17 @@ hipError_t launch_quantize_rows_of(int type, const void *X, int64_t ldx, int64_t
   return hipGetLastError();
 }
 
-template <int MT, int NT, class TY>
+template <int NS, class TY>
 static hipError_t run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const Slices &sl,
-                        const float *bias, TY *Y, hipStream_t s) {
-  const int pairs = sl.n > 1 ? sl.n / 2 : 1;
-  const size_t codes = (size_t)pairs * 2 * 16 * MT * 144;
-  const size_t sums = (size_t)pairs * 2 * NT * MT * 64 * sizeof(float4);
-  auto kern = W.group == 32 ? k_matmul4<32, MT, NT, TY>
-              : W.group == 64 ? k_matmul4<64, MT, NT, TY>
-                              : k_matmul4<128, MT, NT, TY>;
-  const size_t lds = std::max(codes, sums);
-  if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kern),
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-  }
-  hipLaunchKernelGGL(kern, dim3(blocks_for(W.rows, 32 * NT), blocks_for(M, 16 * MT)),
-                     dim3(128 * pairs), lds, s, W, X, M, sl, bias, Y);
+                              const float *bias, TY *Y, hipStream_t s) {
+  const int pairs = sl.n > 1 ? sl.n / 2 : 1, parts = std::min(8 / NS, pairs);
+  const size_t lds =
+      (size_t)parts * 2 * 16 * kMT * kPitch + (size_t)pairs * NS * kMT * 256 * sizeof(float);
+  auto kern = W.group == 32 ? k_matmul4<32, NS, TY>
+              : W.group == 64 ? k_matmul4<64, NS, TY>
+                              : k_matmul4<128, NS, TY>;
+  hipLaunchKernelGGL(kern, dim3(tile_grid(blocks_for(W.rows, 16 * NS), blocks_for(M, 16 * kMT))),
+                     dim3(64 * NS * parts), lds, s, W, X, M, sl, bias, Y);
   return hipGetLastError();
 }
 template <class TY>
@@ -560,17 +654,22 @@ static hipError_t run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const
   while (sl.n < kSlices && 2 * sl.n <= runs) sl.n *= 2;
   sl.per = (runs + sl.n - 1) / sl.n;
   if (M <= 16) {
-    auto kern = W.group == 32 ? k_matmul4_few<32, TY>
-                : W.group == 64 ? k_matmul4_few<64, TY>
-                                : k_matmul4_few<128, TY>;
-    hipLaunchKernelGGL(kern, dim3(blocks_for(W.rows, 16)), dim3(64 * sl.n), 0, s, W, X, M, sl, bias,
-                       Y);
-    return hipGetLastError();
+    auto go = [&](auto rows, auto ahead) {
+      constexpr int R = decltype(rows)::value, A = decltype(ahead)::value;
+      auto kern = W.group == 32 ? k_matmul4_few<32, R, A, TY>
+                  : W.group == 64 ? k_matmul4_few<64, R, A, TY>
+                                  : k_matmul4_few<128, R, A, TY>;
+      hipLaunchKernelGGL(kern, dim3(tile_grid(W.ldr / 16, 1)), dim3(64 * sl.n), 0, s, W, X, M, sl,
+                         bias, Y);
+      return hipGetLastError();
+    };
+    auto by_rows = [&](auto ahead) {
+      return M == 1 ? go(Int<1>(), ahead) : M == 2 ? go(Int<2>(), ahead) : go(Int<4>(), ahead);
+    };
+    return sl.per == 1 ? by_rows(Int<1>()) : sl.per <= 3 ? by_rows(Int<2>()) : by_rows(Int<4>());
   }
-  if (M <= 32) return run_matmul4<2, 1, TY>(W, X, M, sl, bias, Y, s);
-  if (W.ldr >= 32 && W.rows * ((M + 63) / 64) >= 64 * 256)
-    return run_matmul4<4, 2, TY>(W, X, M, sl, bias, Y, s);
-  return run_matmul4<4, 1, TY>(W, X, M, sl, bias, Y, s);
+  return W.rows * ((M + 31) / 32) >= 64 * 256 ? run_matmul4<4>(W, X, M, sl, bias, Y, s)
+                                              : run_matmul4<2>(W, X, M, sl, bias, Y, s);
 }
 hipError_t launch_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, int ytype,
                           void *Y, hipStream_t s) {
