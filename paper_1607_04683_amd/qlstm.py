@@ -903,101 +903,115 @@ def float_layout(H: int, T: int, B: int, backward: bool = False) -> int:
 
 
 # --------------------------------------------- a quantized state-space block
-def _need(t, name, shape, dtype=torch.float32, device=None):
-    """A dense parameter or buffer of the given shape, type and device -> its address."""
+# (The checks are written for their cost: a token's step is a few calls of some
+# microseconds each.)
+def _here(t, name) -> int:
+    """The index of t's GPU, which must be the current one: calls run on its current stream."""
+    i = t.get_device()
+    if i < 0 or i != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} must lie on the current GPU, got {t.device}")
+    return i
+
+
+def _need(t, name, shape, dev, dtype=torch.float32):
+    """A dense parameter or buffer of the given shape (a tuple), GPU and type (or None) -> its
+    address."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: {dtype} {tuple(shape)} wanted, got {t.dtype} {tuple(t.shape)}")
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name}: {dtype} {shape} wanted, got {t.dtype} {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} lies on {t.device}, the other tensors on {device}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} lies on {t.device}, the other tensors on cuda:{dev}")
     return t.data_ptr()
-
-
-def _here(t, name):
-    """The device of t, which must be the current one: calls run on its current stream."""
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} must lie on the current GPU, got {t.device}")
-    return t.device
 
 
 def _rows(t, name, like=None):
     """A matrix with contiguous rows -> (address, leading dimension)."""
     if t is None:
         return None, 0
-    if t.dim() != 2 or t.dtype not in QL_TYPES:
+    if t.dtype not in QL_TYPES or t.dim() != 2:
         raise ValueError(f"{name}: rows of fp32, fp16 or bfloat16 wanted")
     if like is not None and (t.shape != like.shape or t.dtype != like.dtype
-                             or t.device != like.device):
+                             or t.get_device() != like.get_device()):
         raise ValueError(f"{name}: {like.dtype} {tuple(like.shape)} on {like.device} wanted, got "
                          f"{t.dtype} {tuple(t.shape)} on {t.device}")
     m, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError(f"{name}: the values of a row must be contiguous")
-    return t.data_ptr(), t.stride(0) if m > 1 else cols
+    return t.data_ptr(), ld if m > 1 else cols
+
+
+def _qact(q: QAct, m: int, cols: int, dev: int, sums: bool = True) -> CQAct:
+    """The descriptor of m rows of codes of `cols` columns, checked."""
+    shape, codes = (m,), q.codes
+    if q.cols != cols or codes.dim() != 2 or codes.shape[0] != m:
+        raise ValueError(f"codes: {m} rows of {cols} columns wanted")
+    return CQAct(_need(codes, "codes", codes.shape, dev, torch.int8), m, cols, codes.shape[1],
+                 _need(q.zero, "codes' zero points", shape, dev, torch.int32),
+                 _need(q.inv_q, "codes' recovery factors", shape, dev),
+                 _need(q.sums, "codes' sums", shape, dev, torch.int32) if sums else None)
 
 
 def rms_norm(x: torch.Tensor, weight=None, residual=None, eps: float = 1e-6, want=("y",),
              out: dict | None = None) -> dict:
     """ql_rms_norm on rows x [m][cols] -> dict of what `want` names: "y" and "sum"
     (x + residual) of x's type, "codes" (QAct), "rstd" fp32 [m].  out: buffers to use."""
-    dev = _here(x, "x")
+    i = _here(x, "x")
     px, ldx = _rows(x, "x")
-    pr, ldr = _rows(residual, "residual", x)
+    pr, ldr = _rows(residual, "residual", x) if residual is not None else (None, 0)
     m, cols = x.shape
+    dev, empty = x.device, torch.empty
     res = {}
-    for k in want:
+    ps = py = prstd = cq = None
+    lds = ldy = 0
+    for k in want:  # (what is allocated here needs no checks)
         t = out.get(k) if out else None
-        if t is None:
-            if k == "codes":
-                t = QAct(torch.empty(m, ld_for(cols), dtype=torch.int8, device=dev), cols,
-                         torch.empty(m, dtype=torch.int32, device=dev),
-                         torch.empty(m, dtype=torch.float32, device=dev),
-                         torch.empty(m, dtype=torch.int32, device=dev))
-            elif k == "rstd":
-                t = torch.empty(m, dtype=torch.float32, device=dev)
-            elif k in ("y", "sum"):
-                t = torch.empty(m, cols, dtype=x.dtype, device=dev)
+        if k == "codes":
+            if t is None:
+                t = QAct(empty(m, ld_for(cols), dtype=torch.int8, device=dev), cols,
+                         empty(m, dtype=torch.int32, device=dev),
+                         empty(m, dtype=torch.float32, device=dev),
+                         empty(m, dtype=torch.int32, device=dev))
+                cq = CQAct(t.codes.data_ptr(), m, cols, ld_for(cols), t.zero.data_ptr(),
+                           t.inv_q.data_ptr(), t.sums.data_ptr())
             else:
-                raise ValueError(f"want: y, sum, codes and rstd are known, not {k!r}")
+                cq = _qact(t, m, cols, i)
+        elif k == "rstd":
+            if t is None:
+                t = empty(m, dtype=torch.float32, device=dev)
+            prstd = _need(t, "rstd", (m,), i)
+        elif k == "y" or k == "sum":
+            if t is None:
+                t = empty(x.shape, dtype=x.dtype, device=dev)
+                p, ld = t.data_ptr(), cols
+            else:
+                p, ld = _rows(t, k, x)
+            if k == "y":
+                py, ldy = p, ld
+            else:
+                ps, lds = p, ld
+        else:
+            raise ValueError(f"want: y, sum, codes and rstd are known, not {k!r}")
         res[k] = t
-    q, y, s, rstd = res.get("codes"), res.get("y"), res.get("sum"), res.get("rstd")
-    ps, lds = _rows(s, "sum", x)
-    py, ldy = _rows(y, "y", x)
-    cq = None
-    if q is not None:
-        _check_qact(q, m, cols, dev)
-        cq = C.byref(q.cstruct())
     _check(load().ql_rms_norm(QL_TYPES[x.dtype], px, ldx, pr, ldr,
-                              _need(weight, "weight", (cols,), device=dev), m, cols, eps, ps, lds,
-                              py, ldy, cq, _need(rstd, "rstd", (m,), device=dev), _stream()),
-           "ql_rms_norm")
+                              _need(weight, "weight", (cols,), i), m, cols, eps, ps, lds, py, ldy,
+                              cq, prstd, torch._C._cuda_getCurrentRawStream(i)), "ql_rms_norm")
     return res
-
-
-def _check_qact(q: QAct, m: int, cols: int, dev, sums: bool = True):
-    if q.cols != cols or q.codes.dim() != 2 or q.codes.shape[0] != m:
-        raise ValueError(f"codes: {m} rows of {cols} columns wanted")
-    _need(q.codes, "codes", q.codes.shape, torch.int8, dev)
-    _need(q.zero, "codes' zero points", (m,), torch.int32, dev)
-    _need(q.inv_q, "codes' recovery factors", (m,), torch.float32, dev)
-    if sums:
-        _need(q.sums, "codes' sums", (m,), torch.int32, dev)
 
 
 def dequantize_activations(q: QAct) -> torch.Tensor:
     """Recovered rows [m][cols] fp32 of per-vector codes (ql_dequantize, a row a block)."""
-    dev = _here(q.codes, "codes")
-    m = q.codes.shape[0]
-    _check_qact(q, m, q.cols, dev, sums=False)
-    out = torch.empty(m, q.cols, dtype=torch.float32, device=dev)
-    if m == 0:
-        return out
-    cs = CQMatrix(q.codes.data_ptr(), m, q.cols, q.codes.shape[1], m, None, q.zero.data_ptr(),
-                  q.inv_q.data_ptr(), None)
-    _check(load().ql_dequantize(C.byref(cs), out.data_ptr(), _stream()), "ql_dequantize")
+    i = _here(q.codes, "codes")
+    m, cols = q.codes.shape[0], q.cols
+    a = _qact(q, m, cols, i, sums=False)
+    out = torch.empty(m, cols, dtype=torch.float32, device=q.codes.device)
+    if m:
+        cs = CQMatrix(a.codes, m, cols, a.ld, m, None, a.zero, a.inv_q, None)
+        _check(load().ql_dequantize(cs, out.data_ptr(), torch._C._cuda_getCurrentRawStream(i)),
+               "ql_dequantize")
     return out
 
 
@@ -1006,30 +1020,30 @@ def rms_norm_backward(dy: torch.Tensor, v: torch.Tensor, rstd: torch.Tensor, wei
                       workspace: Workspace | None = None):
     """ql_rms_norm_backward -> (dx of dy's type, dweight fp32 [cols] or None).  v: the
     rows that were normed (x, or sum with a residual).  out: buffers "dx", "dweight"."""
-    dev = _here(dy, "dy")
-    m, cols = dy.shape
+    i = _here(dy, "dy")
     pdy, lddy = _rows(dy, "dy")
+    m, cols = dy.shape
     pv, ldv = _rows(v, "v", dy)
-    pds, ldds = _rows(dsum, "dsum", dy)
+    pds, ldds = _rows(dsum, "dsum", dy) if dsum is not None else (None, 0)
     o = out or {}
     dx = o.get("dx")
     if dx is None:
-        dx = torch.empty(m, cols, dtype=dy.dtype, device=dev)
+        dx = torch.empty(m, cols, dtype=dy.dtype, device=dy.device)
     dw = o.get("dweight")
     if dw is None and want_dweight:
-        dw = torch.empty(cols, dtype=torch.float32, device=dev)
+        dw = torch.empty(cols, dtype=torch.float32, device=dy.device)
     pdx, lddx = _rows(dx, "dx", dy)
     lib = load()
     ws = None
     if dw is not None:
-        ws = (workspace or Workspace()).get(lib.ql_rms_norm_backward_workspace(m, cols), dev)
+        ws = (workspace or Workspace()).get(lib.ql_rms_norm_backward_workspace(m, cols), dy.device)
     _check(lib.ql_rms_norm_backward(QL_TYPES[dy.dtype], pdy, lddy, pv, ldv,
-                                    _need(rstd, "rstd", (m,), device=dev),
-                                    _need(weight, "weight", (cols,), device=dev), pds, ldds, m,
-                                    cols, pdx, lddx, _need(dw, "dweight", (cols,), device=dev),
+                                    _need(rstd, "rstd", (m,), i),
+                                    _need(weight, "weight", (cols,), i), pds, ldds, m, cols, pdx,
+                                    lddx, _need(dw, "dweight", (cols,), i),
                                     None if ws is None else ws.data_ptr(),
-                                    0 if ws is None else ws.numel(), _stream()),
-           "ql_rms_norm_backward")
+                                    0 if ws is None else ws.numel(),
+                                    torch._C._cuda_getCurrentRawStream(i)), "ql_rms_norm_backward")
     return dx, dw
 
 
@@ -1049,20 +1063,19 @@ class QMatrix4:
         return 2 * self.codes.shape[1]
 
     def cstruct(self) -> CQMatrix4:
-        c, z, q = self.codes, self.zero, self.inv_q
+        c, z, q, rows, group = self.codes, self.zero, self.inv_q, self.rows, self.group
         ld = 2 * c.shape[1]
-        dims = (ld // self.group if self.group else 0, (self.rows + 15) // 16 * 16)
-        if c.shape[0] != self.rows or z.shape != dims or q.shape != dims:
-            raise ValueError(f"QMatrix4: arrays of other shapes than {self.rows} x {self.cols} in "
-                             f"groups of {self.group} has")
+        dims = (ld // group if group else 0, (rows + 15) // 16 * 16)
+        if c.shape[0] != rows or z.shape != dims or q.shape != dims:
+            raise ValueError(f"QMatrix4: arrays of other shapes than {rows} x {self.cols} in "
+                             f"groups of {group} has")
         if c.dtype != torch.uint8 or z.dtype != torch.int8 or q.dtype != torch.float32:
             raise ValueError("QMatrix4: uint8 codes, int8 zero and float32 inv_q wanted")
         if not (c.is_contiguous() and z.is_contiguous() and q.is_contiguous()):
             raise ValueError("QMatrix4: arrays must be contiguous")
-        if not c.device == z.device == q.device:
+        if not c.get_device() == z.get_device() == q.get_device():
             raise ValueError("QMatrix4: arrays on different devices")
-        return CQMatrix4(c.data_ptr(), self.rows, self.cols, ld, self.group, z.data_ptr(),
-                         q.data_ptr())
+        return CQMatrix4(c.data_ptr(), rows, self.cols, ld, group, z.data_ptr(), q.data_ptr())
 
     @staticmethod
     def empty(rows: int, cols: int, group: int, device) -> "QMatrix4":
@@ -1104,24 +1117,24 @@ class QMatrix4:
 
 def quantize4(W: torch.Tensor, group: int = 64) -> QMatrix4:
     """W [rows][cols] fp32 (device) -> QMatrix4, groups of 32, 64 or 128 columns."""
-    dev = _here(W, "W")
+    i = _here(W, "W")
     if W.dim() != 2 or W.dtype != torch.float32:
         raise ValueError("W: an fp32 matrix wanted")
     if group not in (32, 64, 128):
         raise ValueError("group: 32, 64 or 128")
     W = W.contiguous()
     rows, cols = W.shape
-    q = QMatrix4.empty(rows, cols, group, dev)
-    cs = q.cstruct()
-    _check(load().ql_quantize4(W.data_ptr(), rows, cols, C.byref(cs), _stream()), "ql_quantize4")
+    q = QMatrix4.empty(rows, cols, group, W.device)
+    _check(load().ql_quantize4(W.data_ptr(), rows, cols, q.cstruct(),
+                               torch._C._cuda_getCurrentRawStream(i)), "ql_quantize4")
     return q
 
 
 def dequantize4(q: QMatrix4) -> torch.Tensor:
-    dev = _here(q.codes, "codes")
-    out = torch.empty(q.rows, q.cols, dtype=torch.float32, device=dev)
-    cs = q.cstruct()
-    _check(load().ql_dequantize4(C.byref(cs), out.data_ptr(), _stream()), "ql_dequantize4")
+    i = _here(q.codes, "codes")
+    out = torch.empty(q.rows, q.cols, dtype=torch.float32, device=q.codes.device)
+    _check(load().ql_dequantize4(q.cstruct(), out.data_ptr(),
+                                 torch._C._cuda_getCurrentRawStream(i)), "ql_dequantize4")
     return out
 
 
@@ -1132,45 +1145,46 @@ def matmul4(q: QMatrix4, x, bias=None, out_dtype=None, out: torch.Tensor | None 
     (ql_quantized_matmul4).  Y of out_dtype; by default x's type, fp32 for codes."""
     lib = load()
     cs = q.cstruct()
-    dev = _here(q.codes, "the matrix")
+    i = _here(q.codes, "the matrix")
+    rows, cols = q.rows, q.cols
     act = isinstance(x, QAct)
     if act:
         m = x.codes.shape[0]
-        _check_qact(x, m, q.cols, dev, sums=False)
+        cx = _qact(x, m, cols, i, sums=False)
         dt = out_dtype or torch.float32
     else:
         px, ldx = _rows(x, "x")
         m = x.shape[0]
-        if x.shape[1] != q.cols or x.device != dev:
-            raise ValueError(f"x: rows of {q.cols} columns on {dev} wanted")
+        if x.shape[1] != cols or x.get_device() != i:
+            raise ValueError(f"x: rows of {cols} columns on cuda:{i} wanted")
         dt = out_dtype or x.dtype
     if dt not in QL_TYPES:
         raise ValueError(f"out_dtype: fp32, fp16 or bfloat16 wanted, got {dt}")
     if out is None:
-        out = torch.empty(m, q.rows, dtype=dt, device=dev)
-    py, pb = _need(out, "out", (m, q.rows), dt, dev), _need(bias, "bias", (q.rows,), device=dev)
+        out = torch.empty(m, rows, dtype=dt, device=q.codes.device)
+    py, pb = _need(out, "out", (m, rows), i, dt), _need(bias, "bias", (rows,), i)
+    s = torch._C._cuda_getCurrentRawStream(i)
     if act:
-        cx = x.cstruct()
-        _check(lib.ql_matmul4(C.byref(cs), C.byref(cx), pb, QL_TYPES[dt], py, _stream()),
-               "ql_matmul4")
+        _check(lib.ql_matmul4(cs, cx, pb, QL_TYPES[dt], py, s), "ql_matmul4")
     else:
-        ws = (workspace or Workspace()).get(lib.ql_quantized_matmul4_workspace(m, q.cols), dev)
-        _check(lib.ql_quantized_matmul4(C.byref(cs), QL_TYPES[x.dtype], px, ldx, m, pb,
-                                        QL_TYPES[dt], py, ws.data_ptr(), ws.numel(), _stream()),
-               "ql_quantized_matmul4")
+        ws = (workspace or Workspace()).get(lib.ql_quantized_matmul4_workspace(m, cols),
+                                            q.codes.device)
+        _check(lib.ql_quantized_matmul4(cs, QL_TYPES[x.dtype], px, ldx, m, pb, QL_TYPES[dt], py,
+                                        ws.data_ptr(), ws.numel(), s), "ql_quantized_matmul4")
     return out
 
 
-def _seq(t, name, T, B, width, dtype, dev):
+def _seq(t, name, shape, dtype, dev):
+    """A sequence [T][B][width] with contiguous channels -> its descriptor (or None)."""
     if t is None:
         return None
-    if t.shape != (T, B, width) or t.dtype != dtype or t.device != dev:
-        raise ValueError(f"{name}: {dtype} [{T}][{B}][{width}] on {dev} wanted, got {t.dtype} "
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev:
+        raise ValueError(f"{name}: {dtype} {shape} on cuda:{dev} wanted, got {t.dtype} "
                          f"{tuple(t.shape)} on {t.device}")
     st, sb, sc = t.stride()
-    if width > 1 and sc != 1:
+    if sc != 1 and shape[2] > 1:
         raise ValueError(f"{name}: the channels of a step must be contiguous")
-    return CSeq(t.data_ptr(), st if T > 1 else 0, sb if B > 1 else 0)
+    return CSeq(t.data_ptr(), st if shape[0] > 1 else 0, sb if shape[1] > 1 else 0)
 
 
 def causal_conv(x: torch.Tensor, weight: torch.Tensor, bias=None, silu: bool = True, lengths=None,
@@ -1178,22 +1192,23 @@ def causal_conv(x: torch.Tensor, weight: torch.Tensor, bias=None, silu: bool = T
     """ql_causal_conv: x [T][B][D] (any strides over T and B), weight [width][D], bias [D];
     states [B][width - 1][D] fp32 -> y of x's type and shape.  Rows of a sequence past
     its length are left as they are in `out` (undefined in a new tensor)."""
-    dev = _here(x, "x")
-    if x.dim() != 3 or x.dtype not in QL_TYPES or weight.dim() != 2:
+    i = _here(x, "x")
+    dt = x.dtype
+    if x.dim() != 3 or dt not in QL_TYPES or weight.dim() != 2:
         raise ValueError("x: [T][B][D] of fp32, fp16 or bfloat16, and weight [width][D] wanted")
-    T, B, D = x.shape
+    T, B, D = shape = x.shape
     W = weight.shape[0]
-    cx = _seq(x, "x", T, B, D, x.dtype, dev)
     if out is None:
-        out = torch.empty(T, B, D, dtype=x.dtype, device=dev)
-    cy = _seq(out, "out", T, B, D, x.dtype, dev)
+        out = torch.empty(shape, dtype=dt, device=x.device)
     state = (B, W - 1, D)
-    _check(load().ql_causal_conv(QL_TYPES[x.dtype], cx, _need(weight, "weight", (W, D), device=dev),
-                                 _need(bias, "bias", (D,), device=dev), W, int(bool(silu)), T, B, D,
-                                 _need(lengths, "lengths", (B,), torch.int32, dev),
-                                 _need(state_in, "state_in", state, device=dev),
-                                 _need(state_out, "state_out", state, device=dev), cy, _stream()),
-           "ql_causal_conv")
+    _check(load().ql_causal_conv(QL_TYPES[dt], _seq(x, "x", shape, dt, i),
+                                 _need(weight, "weight", (W, D), i), _need(bias, "bias", (D,), i),
+                                 W, 1 if silu else 0, T, B, D,
+                                 _need(lengths, "lengths", (B,), i, torch.int32),
+                                 _need(state_in, "state_in", state, i),
+                                 _need(state_out, "state_out", state, i),
+                                 _seq(out, "out", shape, dt, i),
+                                 torch._C._cuda_getCurrentRawStream(i)), "ql_causal_conv")
     return out
 
 
@@ -1205,29 +1220,29 @@ def selective_scan(u: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, Bm: to
     type (any strides over T and B), A [states][channels], D and delta_bias [channels] fp32,
     states [B][states][channels] fp32 -> y of u's type.  Rows of a sequence past its
     length are left as they are in `out` (undefined in a new tensor)."""
-    dev = _here(u, "u")
-    if u.dim() != 3 or u.dtype not in QL_TYPES or A.dim() != 2:
+    i = _here(u, "u")
+    dt = u.dtype
+    if u.dim() != 3 or dt not in QL_TYPES or A.dim() != 2:
         raise ValueError("u: [T][B][channels] of fp32, fp16 or bfloat16, and A [states][channels] "
                          "wanted")
-    T, B, ch = u.shape
-    N, dt = A.shape[0], u.dtype
+    T, B, ch = shape = u.shape
+    N = A.shape[0]
+    bc, state = (T, B, N), (B, N, ch)
     if out is None:
-        out = torch.empty(T, B, ch, dtype=dt, device=dev)
-    P = CScan(ch, N, _need(A, "A", (N, ch), device=dev), _need(D, "D", (ch,), device=dev),
-              _need(delta_bias, "delta_bias", (ch,), device=dev), int(bool(softplus)))
+        out = torch.empty(shape, dtype=dt, device=u.device)
+    P = CScan(ch, N, _need(A, "A", (N, ch), i), _need(D, "D", (ch,), i),
+              _need(delta_bias, "delta_bias", (ch,), i), 1 if softplus else 0)
     lib = load()
     nbytes = lib.ql_selective_scan_workspace(ch, N, T, B)
-    ws = (workspace or Workspace()).get(nbytes, dev) if nbytes else None
-    state = (B, N, ch)
-    _check(lib.ql_selective_scan(QL_TYPES[dt], P, _seq(u, "u", T, B, ch, dt, dev),
-                                 _seq(delta, "delta", T, B, ch, dt, dev),
-                                 _seq(Bm, "Bm", T, B, N, dt, dev), _seq(Cm, "Cm", T, B, N, dt, dev),
-                                 _seq(z, "z", T, B, ch, dt, dev), T, B,
-                                 _need(lengths, "lengths", (B,), torch.int32, dev),
-                                 _need(state_in, "state_in", state, device=dev),
-                                 _need(state_out, "state_out", state, device=dev),
-                                 _seq(out, "out", T, B, ch, dt, dev),
+    ws = (workspace or Workspace()).get(nbytes, u.device) if nbytes else None
+    _check(lib.ql_selective_scan(QL_TYPES[dt], P, _seq(u, "u", shape, dt, i),
+                                 _seq(delta, "delta", shape, dt, i), _seq(Bm, "Bm", bc, dt, i),
+                                 _seq(Cm, "Cm", bc, dt, i), _seq(z, "z", shape, dt, i), T, B,
+                                 _need(lengths, "lengths", (B,), i, torch.int32),
+                                 _need(state_in, "state_in", state, i),
+                                 _need(state_out, "state_out", state, i),
+                                 _seq(out, "out", shape, dt, i),
                                  None if ws is None else ws.data_ptr(),
-                                 0 if ws is None else ws.numel(), _stream()),
-           "ql_selective_scan")
+                                 0 if ws is None else ws.numel(),
+                                 torch._C._cuda_getCurrentRawStream(i)), "ql_selective_scan")
     return out
