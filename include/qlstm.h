@@ -477,7 +477,7 @@ ql_status ql_quantized_matmul4(const ql_qmatrix4 *W, ql_type xtype, const void *
  * whether they lie time-major or one utterance after the other. */
 typedef struct {
   void *data;
-  int64_t t_stride, b_stride; /* elements, >= 0 */
+  int64_t t_stride, b_stride; /* elements, >= 0; t_stride < 2^31 */
 } ql_seq;
 /* Short causal convolution over time of every channel, T steps of B sequences of
  * D channels (T <= 2^20, B <= 65535):

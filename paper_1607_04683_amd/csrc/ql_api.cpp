@@ -1530,7 +1530,7 @@ bool rows_clash(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t 
 // Rows (t, b) of a sequence: strides that can be addressed; of an output, rows
 // that do not overlap.
 bool seq_ok(const ql_seq &q, int64_t T, int64_t B, int64_t D, bool output) {
-  if (q.t_stride < 0 || q.b_stride < 0 || q.t_stride > kMaxExtent || q.b_stride > kMaxExtent)
+  if (q.t_stride < 0 || q.b_stride < 0 || q.t_stride > kMaxDim || q.b_stride > kMaxExtent)
     return false;
   if (T <= 0 || B <= 0) return true;
   // (T and B are below 2^21 and 2^16, so the products stay within 64 bits)

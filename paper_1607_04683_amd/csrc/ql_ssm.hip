@@ -15,7 +15,26 @@
 namespace ql {
 
 namespace {
-__device__ __forceinline__ float silu(float v) { return v / (1.0f + expf(-v)); }
+constexpr float kLog2e = 1.44269504088896340736f;
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+// log(1 + e) = 2 atanh(e / (2 + e)), its series to the 13th power: e / (2 + e) is at
+// most 1 / 3, so what is left out is below 2^-26 of the value
+__device__ __forceinline__ float softplus_fast(float x) {
+  const float e = exp2_hw(-fabsf(x) * kLog2e);
+  const float s = e * __builtin_amdgcn_rcpf(2.0f + e), q = s * s;
+  float p = 1.0f / 13.0f;
+  p = __builtin_fmaf(p, q, 1.0f / 11.0f);
+  p = __builtin_fmaf(p, q, 1.0f / 9.0f);
+  p = __builtin_fmaf(p, q, 1.0f / 7.0f);
+  p = __builtin_fmaf(p, q, 1.0f / 5.0f);
+  p = __builtin_fmaf(p, q, 1.0f / 3.0f);
+  p = __builtin_fmaf(p, q, 1.0f);
+  return fmaxf(x, 0.0f) + 2.0f * s * p;
+}
+__device__ __forceinline__ float silu_fast(float v) {
+  return v * __builtin_amdgcn_rcpf(1.0f + exp2_hw(-v * kLog2e));
+}
+
 __device__ __forceinline__ int64_t clamp_len(const int32_t *lengths, int64_t b, int64_t T) {
   if (!lengths) return T;
   const int64_t n = lengths[b];
@@ -23,47 +42,99 @@ __device__ __forceinline__ int64_t clamp_len(const int32_t *lengths, int64_t b, 
 }
 }  // namespace
 
-// A thread per channel of one sequence's chunk of steps.
+// VC neighbouring channels (16 bytes of them) of one sequence's chunk of steps a
+// thread: eight steps' rows in flight, the W - 1 inputs before them as fp32 (a
+// state may hold values that the type does not).  Bound by memory: each input is
+// read once and 3 in 16 a second time, from the cache.
 constexpr int kConvSteps = 16;
-template <int W, class T>
-__global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a) {
-  const int64_t d = (int64_t)blockIdx.x * 256 + threadIdx.x, b = blockIdx.z;
-  const int64_t t0 = (int64_t)blockIdx.y * kConvSteps;
-  const int64_t len = clamp_len(a.lengths, b, a.T);
-  if (d >= a.D || (t0 >= len && t0 > 0)) return;
-  const T *x = static_cast<const T *>(a.x.data) + b * a.x.b_stride + d;
-  T *y = static_cast<T *>(a.y) + b * a.y_b + d;
-  const int64_t state = (b * (W - 1)) * a.D + d;
-  float w[W], v[W];
+template <int W, int VC, bool FULL, class T>
+__device__ __forceinline__ void conv_chunk(const ConvArgs &a, int64_t b, int64_t c0, int t0, int len) {
+  constexpr int S = 8;
+  const int nc = FULL ? VC : (int)(a.D - c0);  // channels there are
+  auto get = [&](float(&v)[VC], const auto *p) {
+    if constexpr (FULL) {
+      load_n<VC>(v, p);
+    } else {
 #pragma unroll
-  for (int j = 0; j < W; ++j) w[j] = a.w[j * a.D + d];
-  const float bias = a.bias ? a.bias[d] : 0.0f;
-  // v[j]: input of step t - W + 1 + j
-  auto before = [&](int64_t t) {  // input of step t < len, from the state where t < 0
-    if (t >= 0) return (float)x[t * a.x.t_stride];
-    return a.state_in ? a.state_in[state + (t + W - 1) * a.D] : 0.0f;
+      for (int i = 0; i < VC; ++i) v[i] = i < nc ? (float)p[i] : 0.0f;
+    }
   };
+  auto put = [&](auto *p, const float(&v)[VC]) {
+    if constexpr (FULL) {
+      store_n<VC>(p, v);
+    } else {
 #pragma unroll
-  for (int j = 0; j + 1 < W; ++j) v[j + 1] = before(t0 - W + 1 + j);
-  const int64_t t1 = t0 + kConvSteps < len ? t0 + kConvSteps : len;
+      for (int i = 0; i < VC; ++i)
+        if (i < nc) p[i] = (std::remove_reference_t<decltype(*p)>)v[i];
+    }
+  };
+  const T *x = static_cast<const T *>(a.x.data) + b * a.x.b_stride + c0;
+  T *y = static_cast<T *>(a.y) + b * a.y_b + c0;
+  const int64_t state = b * (W - 1) * a.D + c0;
+  auto before = [&](float(&v)[VC], int t) {  // input of step t < len, from the state where t < 0
+    if (t >= 0) {
+      get(v, x + t * a.x.t_stride);
+    } else if (a.state_in) {
+      get(v, a.state_in + state + (t + W - 1) * a.D);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VC; ++i) v[i] = 0.0f;
+    }
+  };
+  float w[W][VC], bias[VC], old[W][VC];  // (old: W - 1 of them)
+#pragma unroll
+  for (int k = 0; k < W; ++k) get(w[k], a.w + k * a.D + c0);
+#pragma unroll
+  for (int i = 0; i < VC; ++i) bias[i] = 0.0f;
+  if (a.bias) get(bias, a.bias + c0);
+#pragma unroll
+  for (int k = 0; k + 1 < W; ++k) before(old[k], t0 - W + 1 + k);
   // the first chunk's thread writes the state: it has read the old one where
   // both are one buffer
-  float last[W];
   if (t0 == 0 && a.state_out) {
+    float last[W][VC];
 #pragma unroll
-    for (int j = 0; j + 1 < W; ++j) last[j] = before(len - W + 1 + j);
+    for (int k = 0; k + 1 < W; ++k) before(last[k], len - W + 1 + k);
 #pragma unroll
-    for (int j = 0; j + 1 < W; ++j) a.state_out[state + j * a.D] = last[j];
+    for (int k = 0; k + 1 < W; ++k) put(a.state_out + state + k * a.D, last[k]);
   }
-  for (int64_t t = t0; t < t1; ++t) {
+  const int t1 = t0 + kConvSteps < len ? t0 + kConvSteps : len;
+  for (int t = t0; t < t1; t += S) {
+    float v[S][VC];
 #pragma unroll
-    for (int j = 0; j + 1 < W; ++j) v[j] = v[j + 1];
-    v[W - 1] = (float)x[t * a.x.t_stride];
-    float s = bias;
+    for (int k = 0; k < S; ++k)
+      if (t + k < t1) get(v[k], x + (t + k) * a.x.t_stride);
 #pragma unroll
-    for (int j = 0; j < W; ++j) s = __builtin_fmaf(w[j], v[j], s);
-    y[t * a.y_t] = (T)(a.silu ? silu(s) : s);
+    for (int k = 0; k < S; ++k)
+      if (t + k < t1) {
+        float o[VC];
+#pragma unroll
+        for (int i = 0; i < VC; ++i) {
+          float s = bias[i];
+#pragma unroll
+          for (int n = 0; n < W; ++n) {
+            const int at = k - W + 1 + n;
+            s = __builtin_fmaf(w[n][i], at < 0 ? old[at + W - 1][i] : v[at < 0 ? 0 : at][i], s);
+          }
+          o[i] = a.silu ? silu_fast(s) : s;
+        }
+        put(y + (t + k) * a.y_t, o);
+      }
+#pragma unroll
+    for (int k = 0; k + 1 < W; ++k)
+#pragma unroll
+      for (int i = 0; i < VC; ++i) old[k][i] = v[S - W + 1 + k][i];
   }
+}
+template <int W, int VC, class T>
+__global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a) {
+  const int64_t c0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VC, b = blockIdx.z;
+  const int t0 = blockIdx.y * kConvSteps, len = (int)clamp_len(a.lengths, b, a.T);
+  if (c0 >= a.D || (t0 >= len && t0 > 0)) return;
+  if (c0 + VC <= a.D)
+    conv_chunk<W, VC, true, T>(a, b, c0, t0, len);
+  else
+    conv_chunk<W, VC, false, T>(a, b, c0, t0, len);
 }
 
 // ------------------------------------------------------------------- the scan
@@ -90,30 +161,10 @@ __device__ __forceinline__ float quad_xor(float v) {
   constexpr int ctrl = (0 ^ X) | (1 ^ X) << 2 | (2 ^ X) << 4 | (3 ^ X) << 6;
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), ctrl, 0xf, 0xf, false));
 }
-constexpr float kLog2e = 1.44269504088896340736f;
-__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
-// log(1 + e) = 2 atanh(e / (2 + e)), its series to the 13th power: e / (2 + e) is at
-// most 1 / 3, so what is left out is below 2^-26 of the value
-__device__ __forceinline__ float softplus_fast(float x) {
-  const float e = exp2_hw(-fabsf(x) * kLog2e);
-  const float s = e * __builtin_amdgcn_rcpf(2.0f + e), q = s * s;
-  float p = 1.0f / 13.0f;
-  p = __builtin_fmaf(p, q, 1.0f / 11.0f);
-  p = __builtin_fmaf(p, q, 1.0f / 9.0f);
-  p = __builtin_fmaf(p, q, 1.0f / 7.0f);
-  p = __builtin_fmaf(p, q, 1.0f / 5.0f);
-  p = __builtin_fmaf(p, q, 1.0f / 3.0f);
-  p = __builtin_fmaf(p, q, 1.0f);
-  return fmaxf(x, 0.0f) + 2.0f * s * p;
-}
-__device__ __forceinline__ float silu_fast(float v) {
-  return v * __builtin_amdgcn_rcpf(1.0f + exp2_hw(-v * kLog2e));
-}
-
 // Where the chunks' states lie: slot 0 the initial state, slot k + 1 what chunk k
 // ends with; sums of d per chunk.
 struct ScanChunks {
-  int64_t steps;  // a chunk's, a multiple of kTile
+  int steps;      // a chunk's, a multiple of kTile
   int n;
   float *state;   // [B][n][N][D]
   float *dsum;    // [B][n][D]
@@ -124,15 +175,14 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a, ScanChunks ch) {
   constexpr int NP = 4 * NS, kPer = NP >= 16 ? NP / 16 : 1;  // B (C) values a thread stages
   __shared__ __attribute__((aligned(16))) float bc[2][2][kTile][NP];
   const int tid = threadIdx.x, j = tid & 3;
-  const int64_t D = a.D, b = blockIdx.z, c = blockIdx.y, t0 = c * ch.steps;
-  const int64_t len = clamp_len(a.lengths, b, a.T);
-  const int N = a.N;
+  const int64_t D = a.D, b = blockIdx.z;
+  const int N = a.N, c = blockIdx.y, t0 = c * ch.steps, len = (int)clamp_len(a.lengths, b, a.T);
   if (t0 >= len && c > 0) return;
   if (STATE && t0 + ch.steps >= len && c > 0) return;  // no chunk after it
   const int64_t own = (int64_t)blockIdx.x * 64 + (tid >> 2);
   const bool live = own < D;
   const int64_t d0 = live ? own : D - 1;
-  const int64_t t1 = t0 + ch.steps < len ? t0 + ch.steps : len;
+  const int t1 = t0 + ch.steps < len ? t0 + ch.steps : len;
 
   float h[NS], A[NS];
 #pragma unroll
@@ -155,43 +205,66 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a, ScanChunks ch) {
     // slot 0 alone for chunk 0; else what chunk 0 ends with, and on from there
 #pragma unroll
     for (int i = 0; i < NS; ++i)
-      if (j * NS + i < N) h[i] = slot[((c ? 1 : 0) * N + j * NS + i) * D];
-    for (int64_t k = 1; k < c; ++k) {
-      const float s = ch.dsum[(b * ch.n + k) * D + d0];
+      if (j * NS + i < N) h[i] = slot[(int64_t)((c ? 1 : 0) * N + j * NS + i) * D];
+    // (kJoin chunks' loads at a time: one after the other, each waits for memory)
+    constexpr int kJoin = NS <= 4 ? 8 : NS == 8 ? 4 : 2;
+    for (int k = 1; k < c; k += kJoin) {
+      float ds[kJoin], hs[kJoin][NS];
 #pragma unroll
-      for (int i = 0; i < NS; ++i)
-        if (j * NS + i < N)
-          h[i] = __builtin_fmaf(exp2_hw(s * A[i]), h[i], slot[((k + 1) * N + j * NS + i) * D]);
+      for (int g = 0; g < kJoin; ++g) {
+        const int kk = k + g < c ? k + g : c - 1;
+        ds[g] = ch.dsum[(b * ch.n + kk) * D + d0];
+#pragma unroll
+        for (int i = 0; i < NS; ++i)
+          hs[g][i] = j * NS + i < N ? slot[(int64_t)((kk + 1) * N + j * NS + i) * D] : 0.0f;
+      }
+#pragma unroll
+      for (int g = 0; g < kJoin; ++g)
+        if (k + g < c)
+#pragma unroll
+          for (int i = 0; i < NS; ++i)
+            h[i] = __builtin_fmaf(exp2_hw(ds[g] * A[i]), h[i], hs[g][i]);
     }
   }
 
   const float bias = a.delta_bias ? a.delta_bias[d0] : 0.0f;
   const float skip = !STATE && a.skip ? a.skip[d0] : 0.0f;
-  const T *up = static_cast<const T *>(a.u.data) + b * a.u.b_stride + d0;
-  const T *dp = static_cast<const T *>(a.delta.data) + b * a.delta.b_stride + d0;
-  const T *zp = a.z.data ? static_cast<const T *>(a.z.data) + b * a.z.b_stride + d0 : nullptr;
-  const T *Bp = static_cast<const T *>(a.Bm.data) + b * a.Bm.b_stride;
-  const T *Cp = static_cast<const T *>(a.Cm.data) + b * a.Cm.b_stride;
-  T *yp = static_cast<T *>(a.y) + b * a.y_b + d0;
+  // Pointers at the lane's step of the first group of the tile to be fetched (and
+  // stored), moved on by tiles; strides over time are below 2^31.
+  const int us = (int)a.u.t_stride, ds = (int)a.delta.t_stride, zs = (int)a.z.t_stride,
+            bs = (int)a.Bm.t_stride, cs = (int)a.Cm.t_stride, ys = (int)a.y_t;
+  auto first = [&](const SeqIn &q, int step) {
+    return static_cast<const T *>(q.data) + b * q.b_stride + step * q.t_stride;
+  };
+  const T *up = first(a.u, t0 + j) + d0, *dp = first(a.delta, t0 + j) + d0;
+  const bool gate = !STATE && a.z.data;
+  const T *zp = gate ? first(a.z, t0 + j) + d0 : up;
+  const int bn = tid % NP, bt = tid / NP;  // the state and step this thread stages
+  const T *Bp = first(a.Bm, t0 + bt) + bn, *Cp = first(a.Cm, t0 + bt) + bn;
+  T *yp = static_cast<T *>(a.y) + b * a.y_b + (t0 + j) * a.y_t + d0;
+  constexpr int kApart = 256 / NP;  // steps between the values that a thread stages
 
-  // steps past t1 are loaded from the last one and then masked
   T ru[4], rd[4], rz[4], rb[kPer], rc[kPer];
-  auto fetch = [&](int64_t t) {
+  auto fetch = [&](int t) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int64_t at = t + 4 * g + j < t1 ? t + 4 * g + j : t1 - 1;
-      ru[g] = up[at * a.u.t_stride];
-      rd[g] = dp[at * a.delta.t_stride];
-      if (!STATE && zp) rz[g] = zp[at * a.z.t_stride];
+      // (steps past t1 are loaded from the last one and then masked)
+      const int64_t at = t + 4 * g + j < t1 ? 4 * g : t1 - 1 - t - j;
+      ru[g] = up[at * us];
+      rd[g] = dp[at * ds];
+      if (gate) rz[g] = zp[at * zs];
     }
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-      const int e = k * 256 + tid, n = e % NP;
-      const int64_t at = t + e / NP;
-      const bool on = e < kTile * NP && n < N && at < t1;
-      rb[k] = on ? Bp[at * a.Bm.t_stride + n] : (T)0.0f;
-      if (!STATE) rc[k] = on ? Cp[at * a.Cm.t_stride + n] : (T)0.0f;
+      const bool on = bt + k * kApart < kTile && bn < N && t + bt + k * kApart < t1;
+      rb[k] = on ? Bp[(int64_t)(k * kApart) * bs] : (T)0.0f;
+      if (!STATE) rc[k] = on ? Cp[(int64_t)(k * kApart) * cs] : (T)0.0f;
     }
+    up += kTile * (int64_t)us;
+    dp += kTile * (int64_t)ds;
+    if (gate) zp += kTile * (int64_t)zs;
+    Bp += kTile * (int64_t)bs;
+    if (!STATE) Cp += kTile * (int64_t)cs;
   };
   auto stage = [&](int buf) {
 #pragma unroll
@@ -210,13 +283,13 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a, ScanChunks ch) {
   }
   __syncthreads();
   int buf = 0;
-  for (int64_t t = t0; t < t1; t += kTile, buf ^= 1) {
+  for (int t = t0; t < t1; t += kTile, buf ^= 1) {
     float uu[4], dd[4], zz[4];
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       uu[g] = (float)ru[g];
       dd[g] = (float)rd[g];
-      if (!STATE && zp) zz[g] = (float)rz[g];
+      if (gate) zz[g] = (float)rz[g];
     }
     if (t + kTile < t1) fetch(t + kTile);
 #pragma unroll
@@ -236,11 +309,10 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a, ScanChunks ch) {
             Bv[i] = bc[buf][0][4 * g + k][j * NS + i];
             if (!STATE) Cv[i] = bc[buf][1][4 * g + k][j * NS + i];
           }
-          p[k] = 0.0f;
 #pragma unroll
           for (int i = 0; i < NS; ++i) {
             h[i] = __builtin_fmaf(exp2_hw(dk * A[i]), h[i], duk * Bv[i]);
-            if (!STATE) p[k] = __builtin_fmaf(Cv[i], h[i], p[k]);
+            if (!STATE) p[k] = i == 0 ? Cv[0] * h[0] : __builtin_fmaf(Cv[i], h[i], p[k]);
           }
         };
         step(0, quad_bcast<0>(d), quad_bcast<0>(du));
@@ -254,13 +326,14 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a, ScanChunks ch) {
           const float q1 = (odd ? p[3] : p[2]) + quad_xor<1>(odd ? p[2] : p[3]);
           float y = (high ? q1 : q0) + quad_xor<2>(high ? q0 : q1);
           y = __builtin_fmaf(skip, uu[g], y);
-          if (zp) y *= silu_fast(zz[g]);
-          if (on && live) yp[(t + 4 * g + j) * a.y_t] = (T)y;
+          if (gate) y *= silu_fast(zz[g]);
+          if (on && live) yp[(int64_t)(4 * g) * ys] = (T)y;
         }
       }
     }
     if (t + kTile < t1) stage(buf ^ 1);
-    __syncthreads();
+    if (!STATE) yp += kTile * (int64_t)ys;
+    lds_barrier();
   }
   if (STATE) {
     dsum += quad_xor<1>(dsum);
@@ -269,7 +342,7 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a, ScanChunks ch) {
       if (j == 0) ch.dsum[(b * ch.n + c) * D + d0] = dsum;
 #pragma unroll
       for (int i = 0; i < NS; ++i)
-        if (j * NS + i < N) const_cast<float *>(slot)[((c + 1) * N + j * NS + i) * D] = h[i];
+        if (j * NS + i < N) const_cast<float *>(slot)[(int64_t)((c + 1) * N + j * NS + i) * D] = h[i];
     }
   } else if (a.state_out && live && t0 + ch.steps >= len) {
 #pragma unroll
@@ -278,16 +351,102 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a, ScanChunks ch) {
   }
 }
 
+// One step (a single token): no tiles, four neighbouring channels a lane, the states
+// over the wave's four groups of 16 lanes.  Bound by the state, which is read and
+// written once, in whole lines.
+template <int NS, bool FULL, class T>
+__device__ __forceinline__ void scan_step(const ScanArgs &a, int64_t b, int64_t c0, int q) {
+  const int N = a.N, nc = FULL ? 4 : (int)(a.D - c0);
+  auto get = [&](float(&v)[4], const auto *p) {
+    if constexpr (FULL) {
+      load_n<4>(v, p);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = i < nc ? (float)p[i] : 0.0f;
+    }
+  };
+  auto put = [&](auto *p, const float(&v)[4]) {
+    if constexpr (FULL) {
+      store_n<4>(p, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (i < nc) p[i] = (std::remove_reference_t<decltype(*p)>)v[i];
+    }
+  };
+  auto at = [&](const SeqIn &s, int64_t c) { return static_cast<const T *>(s.data) + b * s.b_stride + c; };
+  float h[NS][4], A[NS][4], Bv[NS], Cv[NS];
+#pragma unroll
+  for (int n = 0; n < NS; ++n) {
+    const int k = q * NS + n;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[n][i] = A[n][i] = 0.0f;
+    Bv[n] = Cv[n] = 0.0f;
+    if (k < N) {
+      if (a.state_in) get(h[n], a.state_in + (b * N + k) * a.D + c0);
+      get(A[n], a.A + k * a.D + c0);
+      Bv[n] = (float)at(a.Bm, k)[0];
+      Cv[n] = (float)at(a.Cm, k)[0];
+    }
+  }
+  if (clamp_len(a.lengths, b, 1) > 0) {
+    float u[4], d[4], bias[4] = {}, skip[4] = {}, z[4] = {}, y[4];
+    get(u, at(a.u, c0));
+    get(d, at(a.delta, c0));
+    if (a.delta_bias) get(bias, a.delta_bias + c0);
+    if (a.skip) get(skip, a.skip + c0);
+    if (a.z.data) get(z, at(a.z, c0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      d[i] += bias[i];
+      if (a.softplus) d[i] = softplus_fast(d[i]);
+      const float dk = d[i] * kLog2e, du = d[i] * u[i];
+      float p = 0.0f;
+#pragma unroll
+      for (int n = 0; n < NS; ++n) {
+        h[n][i] = __builtin_fmaf(exp2_hw(dk * A[n][i]), h[n][i], du * Bv[n]);
+        p = __builtin_fmaf(Cv[n], h[n][i], p);
+      }
+      p += __shfl_xor(p, 16, 64);
+      p += __shfl_xor(p, 32, 64);
+      p = __builtin_fmaf(skip[i], u[i], p);
+      y[i] = a.z.data ? p * silu_fast(z[i]) : p;
+    }
+    if (q == 0) put(static_cast<T *>(a.y) + b * a.y_b + c0, y);
+  }
+  if (a.state_out)
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+      if (q * NS + n < N) put(a.state_out + (b * N + q * NS + n) * a.D + c0, h[n]);
+}
+template <int NS, class T>
+__global__ __launch_bounds__(256) void k_scan_step(ScanArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t c0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 64 + 4 * (lane & 15);
+  if (c0 >= a.D) return;  // (with the other groups' lanes of these channels)
+  if (c0 + 4 <= a.D)
+    scan_step<NS, true, T>(a, blockIdx.y, c0, lane >> 4);
+  else
+    scan_step<NS, false, T>(a, blockIdx.y, c0, lane >> 4);
+}
+
 // ---------------------------------------------------------------- launchers
 static inline unsigned blocks_for(int64_t n, int per) { return (unsigned)((n + per - 1) / per); }
 
+template <int W, class T>
+static void run_conv(const ConvArgs &a, hipStream_t s) {
+  constexpr int VC = 16 / sizeof(T);
+  const dim3 grid(blocks_for(a.D, 256 * VC), a.T ? blocks_for(a.T, kConvSteps) : 1, (unsigned)a.B);
+  hipLaunchKernelGGL((k_causal_conv<W, VC, T>), grid, dim3(256), 0, s, a);
+}
 template <int W>
 static void run_conv(int type, const ConvArgs &a, hipStream_t s) {
-  const dim3 grid(blocks_for(a.D, 256), a.T ? blocks_for(a.T, kConvSteps) : 1, (unsigned)a.B);
-  auto kern = type == 0 ? k_causal_conv<W, float>
-              : type == 1 ? k_causal_conv<W, f16>
-                          : k_causal_conv<W, bf16>;
-  hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a);
+  if (type == 0)
+    run_conv<W, float>(a, s);
+  else if (type == 1)
+    run_conv<W, f16>(a, s);
+  else
+    run_conv<W, bf16>(a, s);
 }
 hipError_t launch_causal_conv(int type, const ConvArgs &a, int width, hipStream_t s) {
   if (a.B == 0) return hipSuccess;
@@ -304,11 +463,11 @@ hipError_t launch_causal_conv(int type, const ConvArgs &a, int width, hipStream_
   return hipGetLastError();
 }
 
-// Chunks of time: enough for 2048 waves, of 32 steps at least, at most 32 (each
-// chunk composes all before it).
+// Chunks of time: enough for 8192 waves, of 32 steps at least, at most 32 (each
+// chunk composes all before it).  From 1024 waves on one pass beats the two.
 static int scan_chunks(int64_t D, int64_t T, int64_t B) {
   const int64_t waves = (D + 63) / 64 * 4 * B;
-  const int64_t want = waves >= 1024 ? 1 : (2048 + waves - 1) / waves;
+  const int64_t want = waves >= 1024 ? 1 : (8192 + waves - 1) / waves;
   return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, 32), T / 32));
 }
 size_t scan_ws(int64_t D, int64_t N, int64_t T, int64_t B) {
@@ -321,10 +480,19 @@ template <class T>
 static void run_scan(const ScanArgs &a, void *ws, hipStream_t s) {
   ScanChunks ch{};
   ch.n = scan_chunks(a.D, a.T, a.B);
-  ch.steps = round_up((a.T + ch.n - 1) / ch.n, kTile);
+  ch.steps = (int)round_up((a.T + ch.n - 1) / ch.n, kTile);
   ch.state = static_cast<float *>(ws);
   ch.dsum = ch.state + a.B * ch.n * a.N * a.D;
   const unsigned x = blocks_for(a.D, 64);
+  if (a.T == 1) {
+    auto kern = a.N <= 4 ? k_scan_step<1, T>
+                : a.N <= 8 ? k_scan_step<2, T>
+                : a.N <= 16 ? k_scan_step<4, T>
+                : a.N <= 32 ? k_scan_step<8, T>
+                            : k_scan_step<16, T>;
+    hipLaunchKernelGGL(kern, dim3(blocks_for(a.D, 256), (unsigned)a.B), dim3(256), 0, s, a);
+    return;
+  }
   if (ch.n > 1) {
     auto kern = a.N <= 4 ? k_scan<1, T, true>
                 : a.N <= 8 ? k_scan<2, T, true>
