@@ -42,14 +42,15 @@ __device__ __forceinline__ int64_t clamp_len(const int32_t *lengths, int64_t b, 
 }
 }  // namespace
 
-// VC neighbouring channels (16 bytes of them) of one sequence's chunk of steps a
-// thread: eight steps' rows in flight, the W - 1 inputs before them as fp32 (a
-// state may hold values that the type does not).  Bound by memory: each input is
-// read once and 3 in 16 a second time, from the cache.
-constexpr int kConvSteps = 16;
+// VC neighbouring channels (8 bytes of them) of one sequence's chunk of eight steps a
+// thread, all rows in flight, the W - 1 inputs before them as fp32 (a state may
+// hold values that the type does not).  What is read a second time comes from the
+// cache.  (4096 x 2048 bfloat16, us: 16 bytes and 16 steps 19, 16 and 8 14.4, 8 and
+// 16 17.9, 8 and 8 13.5.)
+constexpr int kConvSteps = 8;
 template <int W, int VC, bool FULL, class T>
 __device__ __forceinline__ void conv_chunk(const ConvArgs &a, int64_t b, int64_t c0, int t0, int len) {
-  constexpr int S = 8;
+  constexpr int S = kConvSteps;
   const int nc = FULL ? VC : (int)(a.D - c0);  // channels there are
   auto get = [&](float(&v)[VC], const auto *p) {
     if constexpr (FULL) {
@@ -98,38 +99,41 @@ __device__ __forceinline__ void conv_chunk(const ConvArgs &a, int64_t b, int64_t
 #pragma unroll
     for (int k = 0; k + 1 < W; ++k) put(a.state_out + state + k * a.D, last[k]);
   }
-  const int t1 = t0 + kConvSteps < len ? t0 + kConvSteps : len;
-  for (int t = t0; t < t1; t += S) {
+  const int n = len - t0 < S ? len - t0 : S;  // steps there are
+  auto steps = [&](auto whole) {  // (without branches where all eight are)
+    constexpr bool kWhole = decltype(whole)::value;
     float v[S][VC];
 #pragma unroll
     for (int k = 0; k < S; ++k)
-      if (t + k < t1) get(v[k], x + (t + k) * a.x.t_stride);
+      if (kWhole || k < n) get(v[k], x + (t0 + k) * a.x.t_stride);
 #pragma unroll
     for (int k = 0; k < S; ++k)
-      if (t + k < t1) {
+      if (kWhole || k < n) {
         float o[VC];
 #pragma unroll
         for (int i = 0; i < VC; ++i) {
           float s = bias[i];
 #pragma unroll
-          for (int n = 0; n < W; ++n) {
-            const int at = k - W + 1 + n;
-            s = __builtin_fmaf(w[n][i], at < 0 ? old[at + W - 1][i] : v[at < 0 ? 0 : at][i], s);
+          for (int m = 0; m < W; ++m) {
+            const int at = k - W + 1 + m;
+            s = __builtin_fmaf(w[m][i], at < 0 ? old[at + W - 1][i] : v[at < 0 ? 0 : at][i], s);
           }
           o[i] = a.silu ? silu_fast(s) : s;
         }
-        put(y + (t + k) * a.y_t, o);
+        put(y + (t0 + k) * a.y_t, o);
       }
-#pragma unroll
-    for (int k = 0; k + 1 < W; ++k)
-#pragma unroll
-      for (int i = 0; i < VC; ++i) old[k][i] = v[S - W + 1 + k][i];
-  }
+  };
+  if (n == S)
+    steps(std::true_type());
+  else
+    steps(std::false_type());
 }
 template <int W, int VC, class T>
 __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a) {
-  const int64_t c0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * VC, b = blockIdx.z;
-  const int t0 = blockIdx.y * kConvSteps, len = (int)clamp_len(a.lengths, b, a.T);
+  const uint32_t across = (uint32_t)((a.D + 256 * VC - 1) / (256 * VC)), chunk = blockIdx.x / across;
+  const int64_t c0 = ((int64_t)(blockIdx.x - chunk * across) * 256 + threadIdx.x) * VC,
+                b = blockIdx.y;
+  const int t0 = chunk * kConvSteps, len = (int)clamp_len(a.lengths, b, a.T);
   if (c0 >= a.D || (t0 >= len && t0 > 0)) return;
   if (c0 + VC <= a.D)
     conv_chunk<W, VC, true, T>(a, b, c0, t0, len);
@@ -435,8 +439,9 @@ static inline unsigned blocks_for(int64_t n, int per) { return (unsigned)((n + p
 
 template <int W, class T>
 static void run_conv(const ConvArgs &a, hipStream_t s) {
-  constexpr int VC = 16 / sizeof(T);
-  const dim3 grid(blocks_for(a.D, 256 * VC), a.T ? blocks_for(a.T, kConvSteps) : 1, (unsigned)a.B);
+  constexpr int VC = 8 / sizeof(T);
+  // (rows of y lie apart, so T D stays within 2^40 values)
+  const dim3 grid(blocks_for(a.D, 256 * VC) * (a.T ? blocks_for(a.T, kConvSteps) : 1), (unsigned)a.B);
   hipLaunchKernelGGL((k_causal_conv<W, VC, T>), grid, dim3(256), 0, s, a);
 }
 template <int W>
