@@ -1745,6 +1745,13 @@ ql_status ql_quantized_matmul4(const ql_qmatrix4 *W, ql_type xtype, const void *
   if (!X || !Y) return QL_EINVAL;
   if (!ws || ws_bytes < ql_quantized_matmul4_workspace(m, W->cols)) return QL_EWORKSPACE;
   hipStream_t s = as_stream(stream);
+  // in one launch every workgroup reads X while others store Y: only where they lie apart
+  if (!share_bytes(X, (size_t)((m - 1) * ldx + W->cols) * type_size(tx), Y,
+                   (size_t)(m * W->rows) * type_size(ty))) {
+    bool done = false;
+    const hipError_t e = launch_matmul4_rows(weight4(*W), tx, X, ldx, m, W->cols, bias, ty, Y, s, &done);
+    if (e != hipSuccess || done) return from_hip(e);
+  }
   Carve c(ws);
   const ActBuf x = take_act(c, m, W->cols);
   if (launch_quantize_rows_of(tx, X, ldx, m, W->cols, x.codes, x.ld, x.zero, x.inv_q, x.sums, s) !=

@@ -353,6 +353,10 @@ hipError_t launch_dequantize4(const Q4Mat &q, int64_t cols, float *dst, hipStrea
 hipError_t launch_quantize_rows_of(int type, const void *X, int64_t ldx, int64_t m, int64_t K,
                                    int8_t *codes, int64_t ld, int32_t *zero, float *inv_q,
                                    int32_t *sums, hipStream_t s);
+// *done false: more rows or values than one launch should take (nothing launched).
+hipError_t launch_matmul4_rows(const Q4Mat &W, int xtype, const void *X, int64_t ldx, int64_t m,
+                               int64_t cols, const float *bias, int ytype, void *Y, hipStream_t s,
+                               bool *done);
 hipError_t launch_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, int ytype,
                           void *Y, hipStream_t s);
 

@@ -447,6 +447,125 @@ __global__ __launch_bounds__(64 * kSlices) void k_matmul4_few(Q4Mat W, ActRows X
   put4(s, jm, n, W.rows, jq, bias, Y);
 }
 
+// The same from few values of X themselves: every workgroup quantizes them, into LDS,
+// which at these sizes costs less than a launch of its own.
+template <class T>
+struct RowsOf {
+  const T *x;
+  int64_t ld;
+  int cols;
+};
+template <int G, int ROWS, class TX, class TY>
+__global__ __launch_bounds__(64 * kSlices) void k_matmul4_rows(Q4Mat W, RowsOf<TX> X, int M,
+                                                               Slices sl,
+                                                               const float *__restrict__ bias,
+                                                               TY *__restrict__ Y) {
+  constexpr int kAhead = 2, VEC = 16 / sizeof(TX);
+  extern __shared__ __attribute__((aligned(16))) int8_t codes[];  // [M][pitch]
+  __shared__ __attribute__((aligned(16))) float parts[kSlices][16][16];
+  __shared__ int zeros[16];
+  __shared__ float factors[16];
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n0 = tile_of(blockIdx.x, W.ldr / 16, 1).n * 16;
+  if (n0 >= W.rows) return;
+  const int runs = (int)(W.ld / 128), pitch = 128 * runs + 16;
+  const int k0 = wave * sl.per, k1 = k0 + sl.per < runs ? k0 + sl.per : runs;
+  const uint8_t *w = W.codes + n0 * (W.ld / 2);
+  const uint32_t wo = (uint32_t)((n0 + r < W.rows ? r : W.rows - 1 - n0) * (W.ld / 2)) + 16 * q;
+  // the first runs of W are on their way while X is quantized
+  uint4 wv[kAhead][1];
+  RunScales<G, 1> sc[kAhead];
+  auto fetch = [&](int k) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int ku = k + u < runs ? k + u : runs - 1;
+      wv[u][0] = *reinterpret_cast<const uint4 *>((w + 64 * (int64_t)ku) + wo);
+      sc[u].load(W, ku, n0, r);
+    }
+  };
+  fetch(k0);
+  for (int m = wave; m < M; m += blockDim.x >> 6) {
+    const TX *x = X.x + m * X.ld;
+    int8_t *o = codes + m * pitch;
+    float lo = INFINITY, hi = -INFINITY, nan = 0.0f;
+    auto get = [&](float(&v)[VEC], int c) {
+      if (c + VEC <= X.cols) {
+        load_n<VEC>(v, x + c);
+      } else {  // the last value again: it changes no range
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = (float)x[c + i < X.cols ? c + i : X.cols - 1];
+      }
+    };
+    for (int c = VEC * lane; c < X.cols; c += 64 * VEC) {
+      float v[VEC];
+      get(v, c);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        lo = fminf(lo, v[i]);
+        hi = fmaxf(hi, v[i]);
+        nan = __builtin_fmaf(v[i], 0.0f, nan);  // NaN where one is not finite
+      }
+    }
+    lo = wave_min(lo);
+    hi = wave_max(hi);
+    const bool bad = __any(nan != nan);
+    const QParams p = bad ? QParams{0.0, 0, __builtin_nanf(""), 0.0} : make_qparams(lo, hi);
+    const FastEncode f = bad ? FastEncode{0.0f, 0.0f, 2.0f} : fast_encode(p, lo, hi);
+    // (what is coded past the columns meets weights that recover to 0)
+    for (int c = VEC * lane; c < X.cols; c += 64 * VEC) {
+      float v[VEC];
+      get(v, c);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = bad ? 0.0f : v[i];
+      uint32_t words[VEC / 4];
+      encode_words<VEC>(v, p, f, words);
+#pragma unroll
+      for (int i = 0; i < VEC / 4; ++i)
+        reinterpret_cast<uint32_t *>(o + c)[i] = words[i] ^ 0x80808080u;
+    }
+    if (lane == 0) zeros[m] = p.z + 128, factors[m] = p.inv_q;
+  }
+  __syncthreads();
+  int zx[1][ROWS];
+  bool wide = false;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    zx[0][i] = zeros[4 * q + i < M ? 4 * q + i : M - 1];
+    wide |= zx[0][i] != (int)(short)zx[0][i];
+  }
+  wide = __any(wide);
+  const int8_t *xl = codes + (r < M ? r : M - 1) * pitch + 8 * q;
+  float acc[1][1][ROWS];
+  zero_acc(acc);
+  for (int k = k0; k < k1; k += kAhead) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (k + u >= k1) break;
+      int2 xv[1][4];
+#pragma unroll
+      for (int p = 0; p < 4; ++p)
+        xv[0][p] = *reinterpret_cast<const int2 *>(xl + 128 * (k + u) + 32 * p);
+      if (wide)
+        mul4_run<G, 1, 1, ROWS, true>(wv[u], xv, sc[u], zx, acc);
+      else
+        mul4_run<G, 1, 1, ROWS, false>(wv[u], xv, sc[u], zx, acc);
+    }
+    if (k + kAhead < k1) fetch(k + kAhead);
+  }
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) parts[wave][4 * q + i][r] = acc[0][0][i];
+  __syncthreads();
+  const int jm = lane >> 2;
+  const int64_t n = n0 + 4 * (lane & 3);
+  if (wave > 0 || n >= W.rows || jm >= M) return;
+  auto part = [&](int p) { return *reinterpret_cast<const float4 *>(&parts[p][jm][4 * (lane & 3)]); };
+  float4 s = part(0);
+  if (sl.n > 1) s = add4(s, part(1));
+  for (int p = 2; p < sl.n; p += 2) s = add4(s, add4(part(p), part(p + 1)));
+  put4(s, jm, n, W.rows, factors[jm], bias, Y);
+}
+
 // More rows of X: a workgroup takes 16 NS rows of W and 32 of X, its waves NS of rows
 // times the parts that the pairs of slices are shared by.  The NS waves of a part
 // share the codes of X, run by run through LDS, laid out there as the lanes read
@@ -633,6 +752,13 @@ hipError_t launch_quantize_rows_of(int type, const void *X, int64_t ldx, int64_t
   return hipGetLastError();
 }
 
+static Slices slices_of(const Q4Mat &W) {
+  const int runs = (int)(W.ld / 128);
+  Slices sl{1, 0};
+  while (sl.n < kSlices && 2 * sl.n <= runs) sl.n *= 2;
+  sl.per = (runs + sl.n - 1) / sl.n;
+  return sl;
+}
 template <int NS, class TY>
 static hipError_t run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const Slices &sl,
                               const float *bias, TY *Y, hipStream_t s) {
@@ -649,10 +775,7 @@ static hipError_t run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const
 template <class TY>
 static hipError_t run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, TY *Y,
                               hipStream_t s) {
-  const int runs = (int)(W.ld / 128);
-  Slices sl{1, 0};
-  while (sl.n < kSlices && 2 * sl.n <= runs) sl.n *= 2;
-  sl.per = (runs + sl.n - 1) / sl.n;
+  const Slices sl = slices_of(W);
   if (M <= 16) {
     auto go = [&](auto rows, auto ahead) {
       constexpr int R = decltype(rows)::value, A = decltype(ahead)::value;
@@ -677,6 +800,55 @@ hipError_t launch_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const flo
   if (ytype == 0) return run_matmul4(W, X, M, bias, static_cast<float *>(Y), s);
   if (ytype == 1) return run_matmul4(W, X, M, bias, static_cast<f16 *>(Y), s);
   return run_matmul4(W, X, M, bias, static_cast<bf16 *>(Y), s);
+}
+
+// Whether the rows of X and the product should be one launch: it saves the host some
+// 3 us a call, and costs the GPU no more where a wave has at most two short rows to
+// quantize and the workgroups that all do so are few.  Rows x columns x outputs, us a
+// call (us of the GPU's alone) in two launches and in one: 1 x 512 x 2000 11.3 (4.8)
+// and 8.5 (3.6), 1 x 2048 x 8192 11.2 (7.2) and 8.3 (7.5), 1 x 4096 x 2000 11.6 (7.6)
+// and 10.2 (9.8), 4 x 1024 x 8192 11.3 (6.8) and 8.3 (6.4), x 16384 11.4 (8.6) and
+// 10.4 (10.0), 8 x 512 x 8192 12.1 (6.0) and 10.9 (6.0), 16 x 256 x 2000 11.9 (5.0)
+// and 10.9 (9.5), 16 x 1000 x 8192 11.3 (7.9) and 10.8 (10.2).
+static bool one_launch(const Q4Mat &W, int64_t m, int64_t cols) {
+  return m >= 1 && m <= 2 * slices_of(W).n && m * cols <= 4096 && cols <= 2048 && W.rows <= 8192;
+}
+template <class TX, class TY>
+static void run_matmul4_rows(const Q4Mat &W, const RowsOf<TX> &X, int M, const float *bias, TY *Y,
+                             hipStream_t s) {
+  const Slices sl = slices_of(W);
+  auto go = [&](auto rows) {
+    constexpr int R = decltype(rows)::value;
+    auto kern = W.group == 32 ? k_matmul4_rows<32, R, TX, TY>
+                : W.group == 64 ? k_matmul4_rows<64, R, TX, TY>
+                                : k_matmul4_rows<128, R, TX, TY>;
+    hipLaunchKernelGGL(kern, dim3(tile_grid(W.ldr / 16, 1)), dim3(64 * sl.n),
+                       (size_t)M * (size_t)(W.ld + 16), s, W, X, M, sl, bias, Y);
+  };
+  M == 1 ? go(Int<1>()) : go(Int<4>());
+}
+hipError_t launch_matmul4_rows(const Q4Mat &W, int xtype, const void *X, int64_t ldx, int64_t m,
+                               int64_t cols, const float *bias, int ytype, void *Y, hipStream_t s,
+                               bool *done) {
+  *done = one_launch(W, m, cols);
+  if (!*done) return hipSuccess;
+  auto of = [&](auto x) {
+    typedef std::remove_const_t<std::remove_pointer_t<decltype(x)>> TX;
+    const RowsOf<TX> rows{x, ldx, (int)cols};
+    if (ytype == 0)
+      run_matmul4_rows(W, rows, (int)m, bias, static_cast<float *>(Y), s);
+    else if (ytype == 1)
+      run_matmul4_rows(W, rows, (int)m, bias, static_cast<f16 *>(Y), s);
+    else
+      run_matmul4_rows(W, rows, (int)m, bias, static_cast<bf16 *>(Y), s);
+  };
+  if (xtype == 0)
+    of(static_cast<const float *>(X));
+  else if (xtype == 1)
+    of(static_cast<const f16 *>(X));
+  else
+    of(static_cast<const bf16 *>(X));
+  return hipGetLastError();
 }
 
 }  // namespace ql
