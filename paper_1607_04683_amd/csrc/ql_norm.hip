@@ -327,7 +327,7 @@ static void run_rms_norm(const NormArgs &a, hipStream_t s) {
     auto kern = a.cols % VEC == 0 ? k_rms_norm_reg<T, VEC, PER, W, false> : k_rms_norm_reg<T, VEC, PER, W, true>;
     hipLaunchKernelGGL(kern, dim3(blocks_for(a.rows, block_of(W) / (64 * W))), dim3(block_of(W)), 0, s, a);
   };
-  const bool done = a.rows >= 512 ? by_row<true>(a.cols, go) : by_row<false>(a.cols, go);
+  const bool done = deep_rows(a.rows, a.cols) ? by_row<true>(a.cols, go) : by_row<false>(a.cols, go);
   if (!done) hipLaunchKernelGGL(k_rms_norm<T>, dim3((unsigned)a.rows), dim3(256), 0, s, a);
 }
 hipError_t launch_rms_norm(int type, const NormArgs &a, hipStream_t s) {

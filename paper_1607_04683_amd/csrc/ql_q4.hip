@@ -734,7 +734,7 @@ static void run_quantize_rows(const T *X, int64_t ldx, int64_t m, int64_t K, int
     hipLaunchKernelGGL(kern, dim3(blocks_for(m, block_of(W) / (64 * W))), dim3(block_of(W)), 0, s, X,
                        ldx, m, (int)K, codes, ld, zero, inv_q, sums);
   };
-  const bool done = m >= 512 ? by_row<true>(K, go) : by_row<false>(K, go);
+  const bool done = deep_rows(m, K) ? by_row<true>(K, go) : by_row<false>(K, go);
   if (!done)
     hipLaunchKernelGGL(k_quantize_rows_of<T>, dim3(blocks_for(m, 4)), dim3(256), 0, s, X, ldx, m, K,
                        codes, ld, zero, inv_q, sums);
@@ -791,7 +791,10 @@ static hipError_t run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const
     };
     return sl.per == 1 ? by_rows(Int<1>()) : sl.per <= 3 ? by_rows(Int<2>()) : by_rows(Int<4>());
   }
-  return W.rows * ((M + 31) / 32) >= 64 * 256 ? run_matmul4<4>(W, X, M, sl, bias, Y, s)
+  // four waves to the codes of X where 512 workgroups remain, else two and a half of
+  // the rows each (us, with four and with two, groups of 64: 64 x 4096 x 16384 25.5 and
+  // 28.1, x 8192 16.5 and 15.4, 512 x 4096 x 4096 45 and 50, 32 x 4096 x 4096 15.4 and 9.7)
+  return W.rows * ((M + 31) / 32) >= 64 * 512 ? run_matmul4<4>(W, X, M, sl, bias, Y, s)
                                               : run_matmul4<2>(W, X, M, sl, bias, Y, s);
 }
 hipError_t launch_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, int ytype,

@@ -468,12 +468,15 @@ hipError_t launch_causal_conv(int type, const ConvArgs &a, int width, hipStream_
   return hipGetLastError();
 }
 
-// Chunks of time: enough for 8192 waves, of 32 steps at least, at most 32 (each
-// chunk composes all before it).  From 1024 waves on one pass beats the two.
+// Chunks of time: enough for 4096 waves, of 32 steps at least, at most 32 (each
+// chunk composes all before it).  One pass where that fills the chip or the
+// sequence is short (us in one pass and in chunks, B x T x channels of 16 states, fp32:
+// 1 x 64 x 512 12.5 and 14.1, 1 x 128 x 1024 21 and 15.6, 1 x 4096 x 512 554 and 46,
+// 4 x 1000 x 2048 147 and 82, 8 x 1000 x 2048 150 and 142, 16 x 1000 x 2048 217 and 256).
 static int scan_chunks(int64_t D, int64_t T, int64_t B) {
   const int64_t waves = (D + 63) / 64 * 4 * B;
-  const int64_t want = waves >= 1024 ? 1 : (8192 + waves - 1) / waves;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, 32), T / 32));
+  if (waves >= 1536 || T < 96) return 1;
+  return (int)std::min<int64_t>(std::min<int64_t>((4096 + waves - 1) / waves, 32), T / 32);
 }
 size_t scan_ws(int64_t D, int64_t N, int64_t T, int64_t B) {
   if (B == 0) return 0;
