@@ -776,7 +776,13 @@ template <class TY>
 static hipError_t run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, TY *Y,
                               hipStream_t s) {
   const Slices sl = slices_of(W);
-  if (M <= 16) {
+  // A wave a slice and 16 rows of W up to 16 rows of X; but where there are many rows
+  // of W their waves' loads of X weigh more than its way through LDS (us, this way and
+  // through LDS, groups of 64: 1 x 4096 x 16384 12.1 and 14.8, 4 x 4096 x 16384 14.7 and
+  // 15.0, 16 x 4096 x 16384 22.3 and 15.1, x 4096 7.6 and 9.6, 16 x 512 x 16384 4.9
+  // and 5.2).
+  const bool many = M > 4 && W.rows >= 8192 && W.ld >= 1024;
+  if (M <= 16 && !many) {
     auto go = [&](auto rows, auto ahead) {
       constexpr int R = decltype(rows)::value, A = decltype(ahead)::value;
       auto kern = W.group == 32 ? k_matmul4_few<32, R, A, TY>
@@ -789,7 +795,9 @@ static hipError_t run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const
     auto by_rows = [&](auto ahead) {
       return M == 1 ? go(Int<1>(), ahead) : M == 2 ? go(Int<2>(), ahead) : go(Int<4>(), ahead);
     };
-    return sl.per == 1 ? by_rows(Int<1>()) : sl.per <= 3 ? by_rows(Int<2>()) : by_rows(Int<4>());
+    // two runs in flight; one where a slice has no more (16 x 512 x 16384 4.9 us, 7.3
+    // with two).  Four gain nothing (1 x 4096 x 4096 4.8 us, two 4.7).
+    return sl.per == 1 ? by_rows(Int<1>()) : by_rows(Int<2>());
   }
   // four waves to the codes of X where 512 workgroups remain, else two and a half of
   // the rows each (us, with four and with two, groups of 64: 64 x 4096 x 16384 25.5 and
