@@ -403,7 +403,9 @@ ql_status ql_train_step(const ql_train_model *M, const float *feats, const int32
  *
  * A tensor and its neighbours may be column slices of one buffer: `ld` and the
  * strides count elements and are not bound to the widths.  Results must not
- * overlap inputs unless a call says so (QL_EINVAL where it is seen). */
+ * overlap inputs unless a call says so (QL_EINVAL where it is seen).  Calls that
+ * overlap in time (other streams, graphs replayed side by side) need workspaces
+ * of their own, as everywhere in this library. */
 typedef enum { QL_F32 = 0, QL_F16 = 1, QL_BF16 = 2 } ql_type;
 
 /* Root-mean-square norm of m rows of `cols` values (> 0), with the residual's
@@ -463,7 +465,8 @@ ql_status ql_dequantize4(const ql_qmatrix4 *q, float *dst, void *stream);
  * nullable), Y of `type`: the products of a group are summed exactly, the groups
  * in fp32.  X: per-vector codes (X->cols = W->cols, 16-byte aligned; X->sums is
  * not read), from ql_rms_norm or ql_quantize_activations.  Any number of
- * columns; up to 4194240 rows of X. */
+ * columns up to 2^25; up to 4194240 rows of X.  A row of Y does not depend on the
+ * other rows of X, bit for bit. */
 ql_status ql_matmul4(const ql_qmatrix4 *W, const ql_qact *X, const float *bias, ql_type type,
                      void *Y, void *stream);
 /* The same from rows X [m][cols] of xtype, quantized on the fly per row (a row
@@ -497,7 +500,7 @@ ql_status ql_causal_conv(ql_type type, const ql_seq *x, const float *w, const fl
  *   h[n] = exp(d A[n]) h[n] + (d u_t) B_t[n]
  *   y_t = (sum_n C_t[n] h[n] + D u_t) silu(z_t)
  * u, delta, z (nullable: no gate) and y have `channels` values a step, Bm and Cm
- * `states`, shared by the channels.  A [states][channels]; D and delta_bias
+ * `states`, shared by the channels.  A [states][channels], finite; D and delta_bias
  * [channels], nullable (zeros); state [B][states][channels] and lengths as in
  * ql_causal_conv.  y may lie on u, delta or z exactly (same pointer and strides).
  * Chaining calls through the state gives the values of one call to rounding. */

@@ -1578,7 +1578,7 @@ ql_status check_qmatrix4(const ql_qmatrix4 *q) {
   if (!q || !q->codes || !q->zero || !q->inv_q) return QL_EINVAL;
   if (q->rows < 0 || q->cols <= 0 || q->rows > kMaxDim || q->cols > kMaxDim - 127) return QL_ESHAPE;
   if (q->group != 32 && q->group != 64 && q->group != 128) return QL_EUNSUPPORTED;
-  if (q->cols > kMaxCols4) return QL_EUNSUPPORTED;
+  if (q->cols > kMaxCols4 || q->rows * q->ld > kMaxExtent) return QL_EUNSUPPORTED;
   if (q->ld != round_up(q->cols, 128)) return QL_ESHAPE;
   if (!aligned(q->codes, 16) || !aligned(q->inv_q, 16) || !aligned(q->zero, 4)) return QL_EINVAL;
   return QL_OK;
@@ -1586,8 +1586,10 @@ ql_status check_qmatrix4(const ql_qmatrix4 *q) {
 Q4Mat weight4(const ql_qmatrix4 &q) {
   return Q4Mat{q.codes, q.rows, q.ld, q.group, round_up(q.rows, 16), q.zero, q.inv_q};
 }
-// Blocks of 64 rows of X per launch.
-bool matmul4_rows_ok(int64_t m) { return m <= (int64_t)65535 * 64; }
+// Rows of X and results of a product that a launch counts.
+bool matmul4_rows_ok(int64_t m, int64_t rows) {
+  return m <= (int64_t)65535 * 64 && m * rows <= kMaxExtent;
+}
 
 SeqIn seq_in(const ql_seq *q) {
   return q ? SeqIn{q->data, q->t_stride, q->b_stride} : SeqIn{nullptr, 0, 0};
@@ -1716,7 +1718,7 @@ ql_status ql_matmul4(const ql_qmatrix4 *W, const ql_qact *X, const float *bias, 
   const int64_t m = X->rows;
   if (m < 0 || X->cols != W->cols || X->ld % 64 != 0 || !rows_ok(X->ld, m, X->cols))
     return QL_ESHAPE;
-  if (!matmul4_rows_ok(m) || X->ld > kMaxCols4) return QL_EUNSUPPORTED;
+  if (!matmul4_rows_ok(m, W->rows) || X->ld > kMaxCols4) return QL_EUNSUPPORTED;
   if (m == 0 || W->rows == 0) return QL_OK;
   if (!X->codes || !X->zero || !X->inv_q || !Y || !aligned(X->codes, 16)) return QL_EINVAL;
   if (share_bytes(X->codes, (size_t)(m * X->ld), Y, (size_t)(m * W->rows) * type_size(t)))
@@ -1740,7 +1742,7 @@ ql_status ql_quantized_matmul4(const ql_qmatrix4 *W, ql_type xtype, const void *
   const int tx = enum_arg(xtype), ty = enum_arg(ytype);
   if (!type_ok(tx) || !type_ok(ty)) return QL_EINVAL;
   if (m < 0 || !rows_ok(ldx, m, W->cols)) return QL_ESHAPE;
-  if (!matmul4_rows_ok(m)) return QL_EUNSUPPORTED;
+  if (!matmul4_rows_ok(m, W->rows)) return QL_EUNSUPPORTED;
   if (m == 0 || W->rows == 0) return QL_OK;
   if (!X || !Y) return QL_EINVAL;
   if (!ws || ws_bytes < ql_quantized_matmul4_workspace(m, W->cols)) return QL_EWORKSPACE;

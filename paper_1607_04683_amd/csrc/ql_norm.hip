@@ -167,7 +167,10 @@ __global__ __launch_bounds__(256) void k_rms_norm(NormArgs a) {
   }
 }
 
-// Both gradients with the rows in registers: every group of WAVES waves takes rows
+// Both gradients, with x^ = v rstd and g = w dy:
+//   dx = rstd (g - x^ sum(g x^) / n) + dsum,  dweight = sum over rows of dy x^
+// (no power of rstd above the first: rows of zeros with a tiny eps stay finite).
+// The rows lie in registers: every group of WAVES waves takes rows
 // `groups` apart, its share of dweight in registers, which the workgroup adds up
 // and leaves in its row of `part`.  The next row's values are loaded while this
 // one's sum is on its way, where the registers hold both.
@@ -204,18 +207,15 @@ __global__ __launch_bounds__((WAVES == 1 ? 256 : 64 * WAVES)) void k_rms_norm_gr
   }
   for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
     if (a.dsum) get(ds, a.dsum, a.ldds, row);
-    float s = 0.0f;
+    float s = 0.0f, g[PER], xh[PER];
+    const float r0 = rstd;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      dw[i] = __builtin_fmaf(dy[i], v[i] * rstd, dw[i]);
-      dy[i] *= w[i];
-      s = __builtin_fmaf(dy[i], v[i], s);
+      xh[i] = v[i] * r0;
+      dw[i] = __builtin_fmaf(dy[i], xh[i], dw[i]);
+      g[i] = dy[i] * w[i];
+      s = __builtin_fmaf(g[i], xh[i], s);
     }
-    float dx[PER];
-    const float c0 = rstd * rstd * rstd * rn, r0 = rstd;
-    float g[PER], vv[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) g[i] = dy[i] * r0, vv[i] = v[i] * c0;
     const int64_t next = row + step;
     auto load_next = [&] {
       if (next < a.rows) {
@@ -233,9 +233,11 @@ __global__ __launch_bounds__((WAVES == 1 ? 256 : 64 * WAVES)) void k_rms_norm_gr
 #pragma unroll
       for (int q = 1; q < WAVES; ++q) s += ssum[turn][q];
     }
+    s *= rn;
+    float dx[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      dx[i] = __builtin_fmaf(-vv[i], s, g[i]);
+      dx[i] = __builtin_fmaf(-xh[i], s, g[i]) * r0;
       if (a.dsum) dx[i] += ds[i];
     }
     S::template store<TAIL>(static_cast<T *>(a.dx) + row * a.lddx, dx, n, t);
@@ -255,8 +257,7 @@ __global__ __launch_bounds__((WAVES == 1 ? 256 : 64 * WAVES)) void k_rms_norm_gr
   S::template store<TAIL>(part + (int64_t)blockIdx.x * n, dw, n, t);
 }
 
-// dx of one row per workgroup:
-//   dx = rstd g - v rstd^3 / n sum(g v) + dsum,  g = w dy
+// dx of one row per workgroup, rows of any length.
 template <class T>
 __global__ __launch_bounds__(256) void k_rms_norm_dx(NormGradArgs a) {
   __shared__ float ssum[16];
@@ -266,17 +267,16 @@ __global__ __launch_bounds__(256) void k_rms_norm_dx(NormGradArgs a) {
   const T *v = static_cast<const T *>(a.v) + row * a.ldv;
   const T *ds = a.dsum ? static_cast<const T *>(a.dsum) + row * a.ldds : nullptr;
   T *dx = static_cast<T *>(a.dx) + row * a.lddx;
+  const float rstd = a.rstd[row];
   float s = 0.0f;
   for (int64_t i = tid; i < n; i += 256) {
     const float g = a.weight ? a.weight[i] * (float)dy[i] : (float)dy[i];
-    s = __builtin_fmaf(g, (float)v[i], s);
+    s = __builtin_fmaf(g, (float)v[i] * rstd, s);
   }
-  s = block_sum(s, ssum);
-  const float rstd = a.rstd[row];
-  const float c = s * rstd * rstd * rstd / (float)n;
+  s = block_sum(s, ssum) * (1.0f / (float)n);
   for (int64_t i = tid; i < n; i += 256) {
     const float g = a.weight ? a.weight[i] * (float)dy[i] : (float)dy[i];
-    float d = __builtin_fmaf(g, rstd, -((float)v[i] * c));
+    float d = __builtin_fmaf(-((float)v[i] * rstd), s, g) * rstd;
     if (ds) d += (float)ds[i];
     dx[i] = (T)d;
   }

@@ -203,6 +203,53 @@ def test_norm_backward_slices_and_in_place(ql, dtype, m, n, ld, at):
         assert torch.equal(g[k].cpu()[:, keep], bufs[k][:, keep])
 
 
+@pytest.mark.parametrize("n", [70, 20000])
+def test_norm_backward_rows_of_zeros(ql, n):
+    """v = 0 and a tiny eps: dx = rstd w dy (+ dsum), though rstd^3 overflows."""
+    z = gen(9)
+    v, dy, w = torch.zeros(3, n), z(3, n), 1 + 0.1 * z(n)
+    v[1] = z(n)
+    r = ql.rms_norm(v.to(DEV), eps=1e-30, want=("rstd",))["rstd"]
+    dx, dw = ql.rms_norm_backward(dy.to(DEV), v.to(DEV), r, w.to(DEV))
+    want = f64(r)[:, None] * f64(w) * f64(dy)
+    for k in (0, 2):  # two roundings
+        assert (np.abs(f64(dx)[k] - want[k]) <= 2.01 * ref.U32 * np.abs(want[k])).all()
+    assert torch.isfinite(dx).all() and torch.isfinite(dw).all()
+
+
+def test_offsets_past_32_bits(ql):
+    """Rows and steps whose distances in memory pass 2^31 values and 2^32 bytes."""
+    z = gen(10)
+    ld = (1 << 28) - 64
+    buf = torch.empty(12 * ld, dtype=torch.bfloat16, device=DEV)   # 6.4 GB
+    x, w = z(12, 100).bfloat16(), 1 + 0.1 * z(100)
+    rows = buf.as_strided((12, 100), (ld, 1))
+    rows.copy_(x)
+    r = ql.rms_norm(rows, w.to(DEV), want=("y", "sum", "codes", "rstd"), out=dict(y=rows))
+    check_norm(r, x, None, w, 1e-6)
+    rows.copy_(x)
+    q = ql.quantize4((0.1 * z(40, 100)).to(DEV), 32)
+    assert torch.equal(ql.matmul4(q, rows), ql.matmul4(q, x.to(DEV)))
+    seq = buf.as_strided((12, 1, 100), (ld, 100, 1))
+    c = scan_case(12, 1, 100, 4, torch.bfloat16)
+    g = {k: to(v) for k, v in c.items()}
+    seq.copy_(g["u"])
+    kw = dict(D=g["D"], z=g["z"], delta_bias=g["delta_bias"], state_in=g["state"])
+    want = ql.selective_scan(g["u"], g["delta"], g["A"], g["Bm"], g["Cm"], **kw)
+    cw = to(z(4, 100))
+    assert torch.equal(ql.causal_conv(seq, cw), ql.causal_conv(g["u"], cw))
+    y = ql.selective_scan(seq, g["delta"], g["A"], g["Bm"], g["Cm"], out=seq, **kw)
+    assert torch.equal(y, want)
+    del buf, rows, seq, y
+    # results past 2^31 values
+    m, n = 70000, 32768
+    q = ql.quantize4((0.1 * z(n, 32)).to(DEV), 32)
+    X = z(7, 32).repeat(m // 7, 1).to(DEV)
+    Y = ql.matmul4(q, X, out_dtype=torch.bfloat16)
+    assert torch.equal(Y[-7:], ql.matmul4(q, X[:7], out_dtype=torch.bfloat16))
+    assert torch.equal(Y[m // 2 - m // 2 % 7:][:7], Y[:7])
+
+
 def test_norm_backward_no_weight_no_dweight_no_rows(ql):
     z = gen(2)
     v, dy = z(5, 70), z(5, 70)
