@@ -473,21 +473,24 @@ hipError_t launch_causal_conv(int type, const ConvArgs &a, int width, hipStream_
 // sequence is short (us in one pass and in chunks, B x T x channels of 16 states, fp32:
 // 1 x 64 x 512 12.5 and 14.1, 1 x 128 x 1024 21 and 15.6, 1 x 4096 x 512 554 and 46,
 // 4 x 1000 x 2048 147 and 82, 8 x 1000 x 2048 150 and 142, 16 x 1000 x 2048 217 and 256).
-static int scan_chunks(int64_t D, int64_t T, int64_t B) {
-  const int64_t waves = (D + 63) / 64 * 4 * B;
+// Twice as many where sequences may end early: chunks past an end leave at once, and
+// shorter ones spread the rest more evenly (12 x up to 1000 x 1000 99 and 86 us; of
+// full length they cost 3 to 8 %).
+static int scan_chunks(int64_t D, int64_t T, int64_t B, bool ragged) {
+  const int64_t waves = (D + 63) / 64 * 4 * B, want = ragged ? 8192 : 4096;
   if (waves >= 1536 || T < 96) return 1;
-  return (int)std::min<int64_t>(std::min<int64_t>((4096 + waves - 1) / waves, 32), T / 32);
+  return (int)std::min<int64_t>(std::min<int64_t>((want + waves - 1) / waves, 32), T / 32);
 }
 size_t scan_ws(int64_t D, int64_t N, int64_t T, int64_t B) {
   if (B == 0) return 0;
-  const int n = scan_chunks(D, T, B);
+  const int n = scan_chunks(D, T, B, true);
   return n == 1 ? 0 : (size_t)(B * n) * (size_t)((N + 1) * D) * sizeof(float);
 }
 
 template <class T>
 static void run_scan(const ScanArgs &a, void *ws, hipStream_t s) {
   ScanChunks ch{};
-  ch.n = scan_chunks(a.D, a.T, a.B);
+  ch.n = scan_chunks(a.D, a.T, a.B, a.lengths != nullptr);
   ch.steps = (int)round_up((a.T + ch.n - 1) / ch.n, kTile);
   ch.state = static_cast<float *>(ws);
   ch.dsum = ch.state + a.B * ch.n * a.N * a.D;
