@@ -37,6 +37,9 @@ __device__ __forceinline__ F block_sum(F v, F *s) {
 
 // The row in registers: read once.  One wave per row up to 1024 values, four
 // up to 2048, eight up to 4096, 16 up to 16384 (workgroups of four waves at least).
+// Bound by memory: 4096 x 4096 bfloat16 with the sum and codes 29.6 us (117 MB, 4.0 TB/s),
+// 64000 x 500 fp32 39.7 us (256 MB, of which the caches hold a part); short rows of 16
+// bits by the fp64 work once a row (30000 x 333 16.3 us, 2.5 TB/s).
 template <class T, int VEC, int PER, int WAVES, bool TAIL>
 __global__ __launch_bounds__((WAVES == 1 ? 256 : 64 * WAVES)) void k_rms_norm_reg(NormArgs a) {
   typedef RowSlots<VEC, PER, WAVES> S;
@@ -173,7 +176,8 @@ __global__ __launch_bounds__(256) void k_rms_norm(NormArgs a) {
 // The rows lie in registers: every group of WAVES waves takes rows
 // `groups` apart, its share of dweight in registers, which the workgroup adds up
 // and leaves in its row of `part`.  The next row's values are loaded while this
-// one's sum is on its way, where the registers hold both.
+// one's sum is on its way, where the registers hold both.  Bound by memory: 4096 x 4096
+// bfloat16 30.7 us (134 MB, 4.4 TB/s), 12800 x 500 fp32 18.1 us, and 4 us for the join.
 template <class T, int VEC, int PER, int WAVES, bool TAIL>
 __global__ __launch_bounds__((WAVES == 1 ? 256 : 64 * WAVES)) void k_rms_norm_grad(
     NormGradArgs a, float *__restrict__ part) {
