@@ -408,7 +408,7 @@ ql_status ql_train_step(const ql_train_model *M, const float *feats, const int32
  * of their own, as everywhere in this library. */
 typedef enum { QL_F32 = 0, QL_F16 = 1, QL_BF16 = 2 } ql_type;
 
-/* Root-mean-square norm of m rows of `cols` values (> 0), with the residual's
+/* Root-mean-square norm of m rows of `cols` values (1 .. 2^27), with the residual's
  * addition:
  *   v    = x + residual, rounded to the type (residual nullable: v = x)
  *   rstd = (float)(1 / sqrt(sum v^2 / cols + eps)), in fp64; eps >= 0 finite
@@ -447,7 +447,8 @@ ql_status ql_rms_norm_backward(ql_type type, const void *dy, int64_t lddy, const
  * column j in its low half and j + 4 in its high half, each as V' - 8 in two's
  * complement.  Columns [cols, ld) recover to 0.  zero and inv_q:
  * [ld / group][rows rounded up to 16] (the rows past `rows` are not read into
- * any result).  Device memory; codes and inv_q 16-byte, zero 4-byte aligned. */
+ * any result).  At most 2^25 rows and columns, rows x ld at
+ * most 2^34.  Device memory; codes and inv_q 16-byte, zero 4-byte aligned. */
 typedef struct {
   uint8_t *codes;
   int64_t rows, cols, ld;
@@ -464,8 +465,7 @@ ql_status ql_dequantize4(const ql_qmatrix4 *q, float *dst, void *stream);
 /* Y [X->rows][W->rows] = recovered X times recovered W^T (+ bias [W->rows], fp32,
  * nullable), Y of `type`: the products of a group are summed exactly, the groups
  * in fp32.  X: per-vector codes (X->cols = W->cols, 16-byte aligned; X->sums is
- * not read), from ql_rms_norm or ql_quantize_activations.  Any number of
- * columns up to 2^25; up to 4194240 rows of X.  A row of Y does not depend on the
+ * not read), from ql_rms_norm or ql_quantize_activations; up to 4194240 rows of X.  A row of Y does not depend on the
  * other rows of X, bit for bit. */
 ql_status ql_matmul4(const ql_qmatrix4 *W, const ql_qact *X, const float *bias, ql_type type,
                      void *Y, void *stream);
@@ -483,7 +483,7 @@ typedef struct {
   int64_t t_stride, b_stride; /* elements, >= 0; t_stride < 2^31 */
 } ql_seq;
 /* Short causal convolution over time of every channel, T steps of B sequences of
- * D channels (T <= 2^20, B <= 65535):
+ * D channels (T <= 2^20, B <= 65535, D max(T, 1024) <= 2^35):
  *   y_t = f(bias + sum_j w[j] x_{t - width + 1 + j}),  j = 0 .. width - 1 <= 7
  * with f SiLU (silu = 1) or none (0); w [width][D], bias [D] nullable.  state
  * [B][width - 1][D] fp32 holds the last width - 1 inputs, oldest first: state_in
@@ -495,7 +495,7 @@ ql_status ql_causal_conv(ql_type type, const ql_seq *x, const float *w, const fl
                          int32_t width, int32_t silu, int64_t T, int64_t B, int64_t D,
                          const int32_t *lengths, const float *state_in, float *state_out,
                          const ql_seq *y, void *stream);
-/* Selective scan: per channel `states` (1 .. 64) decaying states,
+/* Selective scan: per channel (of up to 2^28) `states` (1 .. 64) decaying states,
  *   d = delta_t + delta_bias, through softplus where asked
  *   h[n] = exp(d A[n]) h[n] + (d u_t) B_t[n]
  *   y_t = (sum_n C_t[n] h[n] + D u_t) silu(z_t)

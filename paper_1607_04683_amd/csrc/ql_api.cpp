@@ -1572,14 +1572,19 @@ bool state_clash(const float *in, const float *out, size_t bytes) {
   return in != out && share_bytes(in, bytes, out, bytes);
 }
 
-// 64 rows of codes stay within 32-bit offsets.
-constexpr int64_t kMaxCols4 = (int64_t)1 << 25;
+// 64 rows of codes stay within 32-bit offsets, and a thread for 8 codes or half of
+// a row within a grid.
+constexpr int64_t kMaxCols4 = (int64_t)1 << 25, kMaxRows4 = kMaxCols4, kMaxCodes4 = (int64_t)1 << 34;
+// Columns of a norm, channels of a scan, channels times steps of a convolution: grids again.
+constexpr int64_t kMaxNormCols = (int64_t)1 << 27, kMaxChannels = (int64_t)1 << 28,
+                  kMaxConv = (int64_t)1 << 35;
 ql_status check_qmatrix4(const ql_qmatrix4 *q) {
   if (!q || !q->codes || !q->zero || !q->inv_q) return QL_EINVAL;
   if (q->rows < 0 || q->cols <= 0 || q->rows > kMaxDim || q->cols > kMaxDim - 127) return QL_ESHAPE;
   if (q->group != 32 && q->group != 64 && q->group != 128) return QL_EUNSUPPORTED;
-  if (q->cols > kMaxCols4 || q->rows * q->ld > kMaxExtent) return QL_EUNSUPPORTED;
   if (q->ld != round_up(q->cols, 128)) return QL_ESHAPE;
+  if (q->cols > kMaxCols4 || q->rows > kMaxRows4 || q->rows * q->ld > kMaxCodes4)
+    return QL_EUNSUPPORTED;
   if (!aligned(q->codes, 16) || !aligned(q->inv_q, 16) || !aligned(q->zero, 4)) return QL_EINVAL;
   return QL_OK;
 }
@@ -1613,6 +1618,7 @@ ql_status ql_rms_norm(ql_type type, const void *x, int64_t ldx, const void *resi
   if (codes && (codes->rows != m || codes->cols != cols || codes->ld % 64 != 0 ||
                 !rows_ok(codes->ld, m, cols)))
     return QL_ESHAPE;
+  if (cols > kMaxNormCols) return QL_EUNSUPPORTED;
   if (m == 0) return QL_OK;
   if (!x) return QL_EINVAL;
   const size_t e = type_size(t);
@@ -1669,6 +1675,7 @@ ql_status ql_rms_norm_backward(ql_type type, const void *dy, int64_t lddy, const
   if (!rows_ok(lddy, m, cols) || !rows_ok(ldv, m, cols) || !rows_ok(lddx, m, cols) ||
       (dsum && !rows_ok(ldds, m, cols)))
     return QL_ESHAPE;
+  if (cols > kMaxNormCols) return QL_EUNSUPPORTED;
   if (m > 0 && (!dy || !v || !rstd || !dx)) return QL_EINVAL;
   const size_t e = type_size(t);
   if (rows_clash(dy, lddy, dx, lddx, m, cols, e) || rows_clash(v, ldv, dx, lddx, m, cols, e) ||
@@ -1769,7 +1776,8 @@ ql_status ql_causal_conv(ql_type type, const ql_seq *x, const float *w, const fl
   const int t = enum_arg(type);
   if (!type_ok(t) || !x || !y || !w || (silu != 0 && silu != 1)) return QL_EINVAL;
   if (T < 0 || B < 0 || D <= 0 || D > kMaxDim || width < 1) return QL_ESHAPE;
-  if (width > 8 || T > kMaxSteps || B > kMaxSequences) return QL_EUNSUPPORTED;
+  if (width > 8 || T > kMaxSteps || B > kMaxSequences || D > kMaxConv / std::max<int64_t>(T, 1024))
+    return QL_EUNSUPPORTED;
   if (!seq_ok(*x, T, B, D, false) || !seq_ok(*y, T, B, D, true)) return QL_ESHAPE;
   if (T * B > 0 && (!x->data || !y->data)) return QL_EINVAL;
   bool same = false;
@@ -1809,7 +1817,7 @@ ql_status ql_selective_scan(ql_type type, const ql_scan *P, const ql_seq *u, con
   if (P->softplus != 0 && P->softplus != 1) return QL_EINVAL;
   const int64_t D = P->channels, N = P->states;
   if (T < 0 || B < 0 || D <= 0 || D > kMaxDim || N < 1) return QL_ESHAPE;
-  if (N > 64 || T > kMaxSteps || B > kMaxSequences) return QL_EUNSUPPORTED;
+  if (N > 64 || T > kMaxSteps || B > kMaxSequences || D > kMaxChannels) return QL_EUNSUPPORTED;
   if (!seq_ok(*u, T, B, D, false) || !seq_ok(*delta, T, B, D, false) ||
       !seq_ok(*Bm, T, B, N, false) || !seq_ok(*Cm, T, B, N, false) ||
       (z && !seq_ok(*z, T, B, D, false)) || !seq_ok(*y, T, B, D, true))

@@ -272,6 +272,8 @@ static bool by_row(int64_t cols, F f) {
 // x 2048 4.5 and 3.9, 512 x 2048 5.7 and 4.7, 1024 x 2048 6.3 and 6.6, 4096 x 4096 28 and
 // 33, 16 x 8000 5.2 and 5.7, 4096 x 8000 52 and 66).
 inline bool deep_rows(int64_t rows, int64_t cols) { return rows >= 1024 || cols > 4096; }
+// A grid has fewer than 2^32 threads: the rows of one launch at `waves` waves a row.
+constexpr int64_t rows_a_launch(int waves) { return ((int64_t)1 << 31) / (64 * waves); }
 constexpr int block_of(int waves) { return waves == 1 ? 256 : 64 * waves; }
 
 // Barrier of a workgroup that orders LDS accesses alone: loads from memory stay in

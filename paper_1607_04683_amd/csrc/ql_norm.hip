@@ -323,15 +323,39 @@ __global__ __launch_bounds__(1024) void k_rms_norm_dw_join(const float *__restri
 // ---------------------------------------------------------------- launchers
 static inline unsigned blocks_for(int64_t n, int per) { return (unsigned)((n + per - 1) / per); }
 
+// Rows [r, r + n) of `all`.
+template <class T>
+static NormArgs norm_rows(const NormArgs &all, int64_t r, int64_t n) {
+  NormArgs a = all;
+  a.rows = n;
+  a.x = static_cast<const T *>(a.x) + r * a.ldx;
+  if (a.residual) a.residual = static_cast<const T *>(a.residual) + r * a.ldr;
+  if (a.sum) a.sum = static_cast<T *>(a.sum) + r * a.lds;
+  if (a.y) a.y = static_cast<T *>(a.y) + r * a.ldy;
+  if (a.rstd) a.rstd += r;
+  if (a.codes) {
+    a.codes += r * a.ldc;
+    a.zero += r;
+    a.inv_q += r;
+    a.sums += r;
+  }
+  return a;
+}
+
 template <class T>
 static void run_rms_norm(const NormArgs &a, hipStream_t s) {
   auto go = [&](auto per, auto w) {
     constexpr int W = decltype(w)::value;
     constexpr int VEC = 16 / sizeof(T), PER = decltype(per)::value;
     auto kern = a.cols % VEC == 0 ? k_rms_norm_reg<T, VEC, PER, W, false> : k_rms_norm_reg<T, VEC, PER, W, true>;
-    hipLaunchKernelGGL(kern, dim3(blocks_for(a.rows, block_of(W) / (64 * W))), dim3(block_of(W)), 0, s, a);
+    for (int64_t r = 0; r < a.rows; r += rows_a_launch(W)) {
+      const int64_t n = std::min(a.rows - r, rows_a_launch(W));
+      hipLaunchKernelGGL(kern, dim3(blocks_for(n, block_of(W) / (64 * W))), dim3(block_of(W)), 0, s,
+                         norm_rows<T>(a, r, n));
+    }
   };
   const bool done = deep_rows(a.rows, a.cols) ? by_row<true>(a.cols, go) : by_row<false>(a.cols, go);
+  // (so many of these long rows that a grid could not hold them, no memory could either)
   if (!done) hipLaunchKernelGGL(k_rms_norm<T>, dim3((unsigned)a.rows), dim3(256), 0, s, a);
 }
 hipError_t launch_rms_norm(int type, const NormArgs &a, hipStream_t s) {

@@ -736,8 +736,12 @@ static void run_quantize_rows(const T *X, int64_t ldx, int64_t m, int64_t K, int
     constexpr int W = decltype(w)::value, VEC = 16 / sizeof(T), PER = decltype(per)::value;
     auto kern = K % VEC == 0 ? k_quantize_rows_reg<T, VEC, PER, W, false>
                              : k_quantize_rows_reg<T, VEC, PER, W, true>;
-    hipLaunchKernelGGL(kern, dim3(blocks_for(m, block_of(W) / (64 * W))), dim3(block_of(W)), 0, s, X,
-                       ldx, m, (int)K, codes, ld, zero, inv_q, sums);
+    for (int64_t r = 0; r < m; r += rows_a_launch(W)) {
+      const int64_t n = std::min(m - r, rows_a_launch(W));
+      hipLaunchKernelGGL(kern, dim3(blocks_for(n, block_of(W) / (64 * W))), dim3(block_of(W)), 0, s,
+                         X + r * ldx, ldx, n, (int)K, codes + r * ld, ld, zero + r, inv_q + r,
+                         sums + r);
+    }
   };
   const bool done = deep_rows(m, K) ? by_row<true>(K, go) : by_row<false>(K, go);
   if (!done)
@@ -813,9 +817,20 @@ static hipError_t run_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const
 hipError_t launch_matmul4(const Q4Mat &W, const ActRows &X, int64_t M, const float *bias, int ytype,
                           void *Y, hipStream_t s) {
   if (M == 0 || W.rows == 0) return hipSuccess;
-  if (ytype == 0) return run_matmul4(W, X, M, bias, static_cast<float *>(Y), s);
-  if (ytype == 1) return run_matmul4(W, X, M, bias, static_cast<f16 *>(Y), s);
-  return run_matmul4(W, X, M, bias, static_cast<bf16 *>(Y), s);
+  auto run = [&](auto *y) {
+    // a grid has fewer than 2^32 threads: at most 512 for 32 rows of W and 32 of X
+    const int64_t across = (int64_t)512 * (W.rows / 32 + 8);
+    const int64_t most = 32 * ((((int64_t)1 << 32) - 1) / across);
+    hipError_t e = hipSuccess;
+    for (int64_t m = 0; m < M && e == hipSuccess; m += most) {
+      const ActRows x{X.codes + m * X.ld, X.ld, X.zero + m, X.inv_q + m, nullptr};
+      e = run_matmul4(W, x, std::min(most, M - m), bias, y + m * W.rows, s);
+    }
+    return e;
+  };
+  if (ytype == 0) return run(static_cast<float *>(Y));
+  if (ytype == 1) return run(static_cast<f16 *>(Y));
+  return run(static_cast<bf16 *>(Y));
 }
 
 // Whether the rows of X and the product should be one launch: it saves the host some

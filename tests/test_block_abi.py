@@ -213,3 +213,29 @@ def test_4bit_layout(ql, rows, cols, group):
         signed = (half.astype(int) ^ 8) - 8
         want = codes[:, k].astype(int) if k < cols else -q.zero.numpy()[k // group, :rows].astype(int)
         assert np.array_equal(signed + 8, want)
+
+
+def test_sizes_past_a_grid(ql):
+    """What no launch can hold is refused before one is tried."""
+    lib, U = ql.load(), ql.QL_EUNSUPPORTED
+    norm = lambda n: lib.ql_rms_norm(0, P, n, None, 0, None, 1, n, 1e-6, None, 0, 8 * P, n, None, None, None)
+    assert norm((1 << 27) + 1) == U
+    n = (1 << 27) + 1
+    assert lib.ql_rms_norm_backward(0, P, n, 8 * P, n, P, None, None, 0, 1, n, 16 * P, n, None, None, 0,
+                                    None) == U
+    big = q4(ql, rows=(1 << 25) + 1)
+    wide = q4(ql, rows=1 << 24, cols=1100, ld=1152)
+    for w in (big, wide):
+        assert lib.ql_quantize4(P, w.rows, w.cols, C.byref(w), None) == U
+        assert lib.ql_dequantize4(C.byref(w), P, None) == U
+    # a leading dimension whose extent passes 64 bits is a wrong one
+    assert lib.ql_dequantize4(C.byref(q4(ql, rows=1 << 24, ld=1 << 62)), P, None) == ql.QL_ESHAPE
+    D = (1 << 25) + 1
+    conv = lib.ql_causal_conv(0, seq(ql, P, D, D), P, None, 4, 1, 1, 1, D, None, None, None,
+                              seq(ql, 8 * P, D, D), None)
+    assert conv == U
+    D = (1 << 28) + 1
+    q = seq(ql, P, D, D)
+    assert lib.ql_selective_scan(0, ql.CScan(D, 1, P, None, None, 1), q, q, seq(ql, P, 1, 1),
+                                 seq(ql, P, 1, 1), None, 1, 1, None, None, None, seq(ql, 8 * P, D, D), None,
+                                 0, None) == U

@@ -601,3 +601,24 @@ def test_scan_extremes(ql):
     on[20:, 0, 3] = False
     assert torch.isnan(a[100:, 1, 7]).all()
     ref.close(a[on], y[on.numpy()], by[on.numpy()], torch.float32, "others")
+
+
+def test_rows_past_a_launch(ql):
+    """More rows than one grid holds: the rows on both sides of the cuts."""
+    m = (1 << 25) + 70
+    at = (0, (1 << 25) - 3, m - 5)
+    x = torch.randn(m, 1, device=DEV)
+    r = ql.rms_norm(x, torch.ones(1, device=DEV) * 1.5, eps=0.1, want=("y", "rstd"))
+    for i in at:
+        part = ql.rms_norm(x[i:i + 5].clone(), torch.ones(1, device=DEV) * 1.5, eps=0.1, want=("y", "rstd"))
+        assert torch.equal(r["y"][i:i + 5], part["y"]) and torch.equal(r["rstd"][i:i + 5], part["rstd"])
+    del x, r
+    m, n = 2_000_003, 4096
+    w = ql.quantize4(torch.randn(n, 32, device=DEV), 32)
+    x = torch.randn(m, 32, device=DEV)
+    bias = torch.randn(n, device=DEV)
+    y = ql.matmul4(w, x, bias, out_dtype=torch.bfloat16)
+    cut = 32 * (((1 << 32) - 1) // (512 * (n // 32 + 8)))
+    assert cut < m
+    for i in (0, cut - 3, m - 5):
+        assert torch.equal(y[i:i + 5], ql.matmul4(w, x[i:i + 5].clone(), bias, out_dtype=torch.bfloat16))
